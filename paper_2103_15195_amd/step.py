@@ -1,0 +1,205 @@
+"""Binding of the operators around a step's exchange of gradients (the C ABI in include/mergecomp_step.h): the global
+gradient norm, clipping and AdamW over a model's list of tensors, token log-probabilities and the clipped policy loss
+over rows of logits.
+
+Like binding.py it marshals arguments only, tensors are passed by ``data_ptr()`` and ``stream=None`` is torch's current
+stream.  Tensors are checked where they are handed over, since the kernels go by sizes that are fixed then.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Sequence, Tuple
+
+from . import binding as B
+
+MC_DTYPE_NONE, MC_DTYPE_F32, MC_DTYPE_BF16, MC_DTYPE_F16 = -1, 0, 1, 2
+DTYPE_IDS = {"float32": 0, "bfloat16": 1, "float16": 2}
+LISTS = {"grads": 0, "clipped": 1, "params": 2, "exp_avg": 3, "exp_avg_sq": 4, "model": 5}
+
+EXPORTS = ["mc_step_create", "mc_step_destroy", "mc_step_bind", "mc_grad_norm", "mc_grad_clip", "mc_adamw",
+           "mc_loss_create", "mc_loss_destroy", "mc_token_logp", "mc_policy_loss"]
+
+
+class McAdamwConfig(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("step", C.c_int64)]
+
+
+class McLogits(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("labels", C.c_void_p), ("rows", C.c_int64), ("vocab", C.c_int64), ("stride", C.c_int64),
+                ("dtype", C.c_int32), ("temperature", C.c_float)]
+
+
+class McPolicy(C.Structure):
+    _fields_ = [("old_logp", C.c_void_p), ("advantages", C.c_void_p), ("weights", C.c_void_p), ("ref_logp", C.c_void_p),
+                ("clip_low", C.c_float), ("clip_high", C.c_float), ("kl_coef", C.c_float), ("grad_scale", C.c_float),
+                ("sums", C.c_void_p), ("logp", C.c_void_p), ("dlogits", C.c_void_p), ("dlogits_stride", C.c_int64)]
+
+
+_declared = None
+
+
+def lib():
+    """The loaded library with these operators' signatures."""
+    global _declared
+    L = B.lib()
+    if _declared is not L:
+        vp, i32, f32 = C.c_void_p, C.c_int32, C.c_float
+        L.mc_step_create.argtypes = [C.POINTER(vp), vp, i32, i32, i32, vp]
+        L.mc_step_destroy.argtypes = [vp]
+        L.mc_step_bind.argtypes = [vp, i32, vp, vp]
+        L.mc_grad_norm.argtypes = [vp, f32, f32, vp, vp]
+        L.mc_grad_clip.argtypes = [vp, f32, f32, vp, vp]
+        L.mc_adamw.argtypes = [vp, C.POINTER(McAdamwConfig), vp, vp]
+        L.mc_loss_create.argtypes = [C.POINTER(vp)]
+        L.mc_loss_destroy.argtypes = [vp]
+        L.mc_token_logp.argtypes = [vp, C.POINTER(McLogits), vp, vp]
+        L.mc_policy_loss.argtypes = [vp, C.POINTER(McLogits), C.POINTER(McPolicy), vp]
+        _declared = L
+    return L
+
+
+def dtype_id(dtype) -> int:
+    """mc_dtype of a torch dtype or its name; None: no type."""
+    if dtype is None:
+        return MC_DTYPE_NONE
+    name = str(dtype).replace("torch.", "")
+    if name not in DTYPE_IDS:
+        raise ValueError(f"{dtype}: one of {', '.join(DTYPE_IDS)}")
+    return DTYPE_IDS[name]
+
+
+def _kind(tensor) -> str:
+    return str(tensor.dtype).replace("torch.", "")
+
+
+def _vector(tensor, name: str, count: int, kind: str = "float32"):
+    """The address of a contiguous device tensor of `count` elements."""
+    if not tensor.is_cuda or _kind(tensor) != kind or tensor.numel() != count or not tensor.is_contiguous():
+        raise ValueError(f"{name}: {count} contiguous {kind} values on the device, not {tuple(tensor.shape)} of {tensor.dtype} on {tensor.device}")
+    return tensor.data_ptr()
+
+
+class Step:
+    """One model's list of tensors on the current device: wraps mc_step.
+
+    grad_dtype   type of the gradients (and of what mc_grad_clip writes)
+    model_dtype  type of the copy of the weights that the model computes with, or None for no such copy
+    no_decay     per tensor, whether weight decay leaves it out
+    """
+
+    def __init__(self, numel: Sequence[int], grad_dtype="float32", model_dtype=None, no_decay: Optional[Sequence[bool]] = None):
+        self.numel = [int(n) for n in numel]
+        n = len(self.numel)
+        if no_decay is not None and len(no_decay) != n:
+            raise ValueError(f"no_decay: one entry for each of the {n} tensors")
+        if model_dtype is not None and dtype_id(model_dtype) == MC_DTYPE_F32:
+            raise ValueError("model_dtype: 16 bits, or None (the weights themselves are 32 bits)")
+        self.dtypes = {"grads": dtype_id(grad_dtype), "clipped": dtype_id(grad_dtype), "model": dtype_id(model_dtype),
+                       "params": MC_DTYPE_F32, "exp_avg": MC_DTYPE_F32, "exp_avg_sq": MC_DTYPE_F32}
+        self._kept = {}
+        self._h = C.c_void_p()
+        nm = (C.c_int64 * max(n, 1))(*self.numel)
+        nd = None if no_decay is None else (C.c_uint8 * max(n, 1))(*[1 if x else 0 for x in no_decay])
+        B._check(lib().mc_step_create(C.byref(self._h), nm, n, self.dtypes["grads"], self.dtypes["model"], nd), "mc_step_create")
+
+    def close(self) -> None:
+        if getattr(self, "_h", None):
+            lib().mc_step_destroy(self._h)
+            self._h = None
+            self._kept = {}
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def bind(self, stream=None, **lists) -> None:
+        """Hands over lists of tensors, one tensor for each of the model: grads, clipped, params, exp_avg, exp_avg_sq, model.
+        A list holds until it is handed over again; its tensors are kept alive until then."""
+        for name, tensors in lists.items():
+            if name not in LISTS:
+                raise ValueError(f"{name}: one of {', '.join(LISTS)}")
+            if name == "model" and self.dtypes["model"] == MC_DTYPE_NONE:
+                raise ValueError("model: the handle was made without a model_dtype")
+            tensors = list(tensors)
+            if len(tensors) != len(self.numel):
+                raise ValueError(f"{name}: {len(self.numel)} tensors, not {len(tensors)}")
+            for i, (t, n) in enumerate(zip(tensors, self.numel)):
+                if t.numel() != n or not t.is_contiguous() or not t.is_cuda or DTYPE_IDS.get(_kind(t)) != self.dtypes[name]:
+                    raise ValueError(f"{name}[{i}]: {n} contiguous elements on the device of the list's type, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+        for name, tensors in lists.items():
+            tensors = list(tensors)
+            B._check(lib().mc_step_bind(self._h, LISTS[name], B.ptr_array(tensors), B._stream_handle(stream)), "mc_step_bind")
+            self._kept[name] = tensors
+
+    def mc_grad_norm(self, max_norm: float, out, scale: float = 1.0, stream=None) -> None:
+        """out: two floats on the device, the norm of scale * gradients and the coefficient that clips them to max_norm."""
+        B._check(lib().mc_grad_norm(self._h, scale, max_norm, _vector(out, "out", 2), B._stream_handle(stream)), "mc_grad_norm")
+
+    def mc_grad_clip(self, max_norm: float, out, scale: float = 1.0, stream=None) -> None:
+        """mc_grad_norm, and the gradients times the coefficient into the list `clipped`, or in place where it is not bound."""
+        B._check(lib().mc_grad_clip(self._h, scale, max_norm, _vector(out, "out", 2), B._stream_handle(stream)), "mc_grad_clip")
+
+    def mc_adamw(self, step: int, lr: float, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
+                 coef=None, stream=None) -> None:
+        """coef: one float on the device that the gradients are multiplied by, such as the second of mc_grad_norm."""
+        cfg = McAdamwConfig(lr, betas[0], betas[1], eps, weight_decay, step)
+        B._check(lib().mc_adamw(self._h, C.byref(cfg), None if coef is None else _vector(coef, "coef", 1), B._stream_handle(stream)), "mc_adamw")
+
+
+class PolicyLoss:
+    """Scratch of the calls over rows of logits, on the current device: wraps mc_loss."""
+
+    def __init__(self):
+        self._h = C.c_void_p()
+        B._check(lib().mc_loss_create(C.byref(self._h)), "mc_loss_create")
+
+    def close(self) -> None:
+        if getattr(self, "_h", None):
+            lib().mc_loss_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    @staticmethod
+    def _rows(x, name: str):
+        """(rows, columns, elements from row to row) of a two-dimensional tensor whose rows are contiguous."""
+        if x.dim() != 2 or not x.is_cuda or _kind(x) not in DTYPE_IDS or (x.shape[1] > 1 and x.stride(1) != 1):
+            raise ValueError(f"{name}: rows of contiguous values on the device, of {', '.join(DTYPE_IDS)}, not {tuple(x.shape)} of {x.dtype} on {x.device}")
+        rows, columns = x.shape
+        return rows, columns, x.stride(0) if rows > 1 else max(x.stride(0), columns)
+
+    def _logits(self, logits, labels, temperature):
+        rows, vocab, stride = self._rows(logits, "logits")
+        return McLogits(logits.data_ptr(), _vector(labels, "labels", rows, "int64"), rows, vocab, stride, DTYPE_IDS[_kind(logits)], temperature)
+
+    def mc_token_logp(self, logits, labels, logp, temperature: float = 1.0, stream=None) -> None:
+        """logp[r] = log-probability of labels[r] under logits[r] / temperature; 0 where the label is none of the row's."""
+        x = self._logits(logits, labels, temperature)
+        B._check(lib().mc_token_logp(self._h, C.byref(x), _vector(logp, "logp", x.rows), B._stream_handle(stream)), "mc_token_logp")
+
+    def mc_policy_loss(self, logits, labels, old_logp, advantages, *, sums, weights=None, ref_logp=None, clip: Tuple[float, float] = (0.2, 0.2),
+                       kl_coef: float = 0.0, temperature: float = 1.0, grad_scale: float = 1.0, logp=None, dlogits=None, stream=None) -> None:
+        """The loss of mergecomp_step.h and, in dlogits (which may be the logits), grad_scale times its gradient.
+        sums: 8 floats on the device: loss, policy term, KL term, clipped weight, weight; as int32 rows that took part, rows
+        whose label is none of the row's; 0."""
+        x = self._logits(logits, labels, temperature)
+        n, p = x.rows, McPolicy()
+        p.old_logp, p.advantages = _vector(old_logp, "old_logp", n), _vector(advantages, "advantages", n)
+        p.weights = None if weights is None else _vector(weights, "weights", n)
+        p.ref_logp = None if ref_logp is None else _vector(ref_logp, "ref_logp", n)
+        p.clip_low, p.clip_high, p.kl_coef, p.grad_scale = clip[0], clip[1], kl_coef, grad_scale
+        p.sums = _vector(sums, "sums", 8)
+        p.logp = None if logp is None else _vector(logp, "logp", n)
+        if dlogits is not None:
+            rows, vocab, p.dlogits_stride = self._rows(dlogits, "dlogits")
+            if (rows, vocab) != (x.rows, x.vocab) or dlogits.dtype != logits.dtype:
+                raise ValueError(f"dlogits: the logits' shape and type, not {tuple(dlogits.shape)} of {dlogits.dtype}")
+            p.dlogits = dlogits.data_ptr()
+        B._check(lib().mc_policy_loss(self._h, C.byref(x), C.byref(p), B._stream_handle(stream)), "mc_policy_loss")
