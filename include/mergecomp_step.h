@@ -102,7 +102,7 @@ int mc_adamw(mc_step *h, const mc_adamw_config *cfg, const float *coef, void *st
 /* ---- rows of logits ------------------------------------------------------------------------------------------- */
 typedef struct mc_loss mc_loss;
 
-/* Scratch for the calls below on the current HIP device (about 150 KB). */
+/* Scratch for the calls below on the current HIP device (2 MB). */
 int mc_loss_create(mc_loss **out);
 int mc_loss_destroy(mc_loss *h);
 

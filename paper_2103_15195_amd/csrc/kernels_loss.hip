@@ -3,6 +3,8 @@
 
 namespace mc {
 
+constexpr float kNone = -__builtin_inff();
+
 // exp((x - top) / temperature) for logits of type T.  The difference comes first, so that a row of nothing but the type's lowest
 // value is as good as any other.  With logits of 32 bits the factor has a second part: rounded to 24 bits it moves
 // exp(-10) by 4e-7 (what is infinite already stays away from that part: times 0 or a negative number it would be NaN).
@@ -14,55 +16,348 @@ __device__ __forceinline__ float row_exp(const LossArgs &a, float x, float top)
     return __builtin_amdgcn_exp2f(__builtin_fmaf(d, a.to_base2, fmaxf(d, -1e30f) * a.to_base2_rest));
 }
 // where a maximum of minus infinity (nothing seen so far) stands for exponents: any finite number
-__device__ __forceinline__ float base_of(float top) { return top == -__builtin_inff() ? 0.0f : top; }
+__device__ __forceinline__ float base_of(float top) { return top == kNone ? 0.0f : top; }
+// log(x), x >= 0, beyond binary32: the exponent and the logarithm of what is between 1/2 and 1
+__device__ __forceinline__ double log_wide(float x)
+{
+    if (!(x > 0.0f && x < __builtin_inff())) return (double)logf(x);
+    int e;
+    const float f = frexpf(x, &e);
+    return (double)e * 0.693147180559945309 + (double)logf(f);
+}
 
-// What a row adds to the sums, and the slope of its loss by its log-probability.
-struct RowTerms { float policy, kl, cut, slope; };
-__device__ __forceinline__ RowTerms row_terms(const LossArgs &a, uint32_t r, float logp)
+__device__ __forceinline__ float wave_sum_f(float x)
+{
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, 64);
+    return x;
+}
+
+// What a row is besides its logits.  A row's number is the same for a wavefront, and what is looked up by it comes through the scalar
+// cache and stays in scalar registers.
+struct Row {
+    int64_t label;
+    float weight;
+    __device__ __forceinline__ bool valid(const LossArgs &a) const { return label >= 0 && label < (int64_t)a.vocab; }
+    __device__ __forceinline__ bool taken(const LossArgs &a) const { return valid(a) && weight != 0.0f; }
+};
+template <bool LOSS>
+__device__ __forceinline__ Row row_of(const LossArgs &a, uint32_t r)
+{
+    Row row{ld_uniform(a.labels + r), 1.0f};
+    if (LOSS && a.weights) row.weight = ld_uniform(a.weights + r);
+    return row;
+}
+
+// What a row adds to the sums, and the slope of its loss by its log-probability l.
+struct RowTerms { float policy, kl, slope; bool cut; };
+__device__ __forceinline__ RowTerms row_terms(const LossArgs &a, uint32_t r, double l)
 {
     RowTerms t;
-    const float adv = a.advantages[r], rho = expf(logp - a.old_logp[r]);
+    const float adv = ld_uniform(a.advantages + r), rho = expf((float)(l - (double)ld_uniform(a.old_logp + r)));
     const float free = -adv * rho, held = -adv * fminf(fmaxf(rho, a.lo), a.hi);
     const bool is_free = !(free < held);              // (NaN: the ratio's)
     t.policy = is_free ? free : held;
     t.slope = is_free ? free : 0.0f;
-    t.cut = is_free ? 0.0f : 1.0f;
+    t.cut = !is_free;
     t.kl = 0.0f;
     if (a.ref_logp) {
-        const float d = a.ref_logp[r] - logp, ed = expf(d);
+        const float d = (float)((double)ld_uniform(a.ref_logp + r) - l), ed = expf(d);
         t.kl = ed - d - 1.0f;
         t.slope += a.kl_coef * (1.0f - ed);
     }
     return t;
 }
 
-// One block to a row, two passes over it: the running maximum and sum, then the gradient.
-template <class T, bool LOSS>
-__global__ __launch_bounds__(kBlock) void loss_rows_k(LossArgs a)
+// ---- sums over rows ---------------------------------------------------------------------------------------------------
+// The rows' kernels leave a Term for every row.  In launches of few blocks the last one adds them up; in larger ones, where that
+// block would find thousands of them and every block would wait for its terms to be written through, a kernel behind them does.
+struct Sums {
+    double at[kLossSums] = {};
+    __device__ __forceinline__ void add(const Term &t, float kl_coef)
+    {
+        const bool taken = t.kind == TERM_FREE || t.kind == TERM_CUT;
+        const double w = taken ? (double)t.weight : 0.0;
+        if (taken) {
+            at[0] += w * ((double)t.policy + (double)kl_coef * t.kl);
+            at[1] += w * t.policy;
+            at[2] += w * t.kl;
+        }
+        at[3] += t.kind == TERM_CUT ? w : 0.0;
+        at[4] += w;
+        at[5] += taken ? 1.0 : 0.0;
+        at[6] += t.kind == TERM_LEFT_OUT ? 1.0 : 0.0;
+    }
+    __device__ __forceinline__ void join()
+    {
+#pragma unroll
+        for (int k = 0; k < kLossSums; ++k) at[k] = wave_sum(at[k]);
+    }
+    __device__ __forceinline__ void put(float *out) const
+    {
+#pragma unroll
+        for (int k = 0; k < kLossSums; ++k) out[k] = k < 5 ? (float)at[k] : __int_as_float((int)at[k]);
+        out[kLossSums] = 0.0f;
+    }
+};
+// a term past the caches, to a block that may sit on another die, and there
+__device__ __forceinline__ void leave_term(Term *to, const Term &t)
 {
-    constexpr int N = 16 / (int)sizeof(T);
-    __shared__ float lds[2 * kWavesPerBlock];
-    double sums[kLossSums] = {};
-    for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const int64_t label = a.labels[r];
-        const float w = LOSS ? (a.weights ? a.weights[r] : 1.0f) : 1.0f;
-        const bool valid = label >= 0 && label < (int64_t)a.vocab, taken = valid && w != 0.0f;
+    const uint64_t *from = reinterpret_cast<const uint64_t *>(&t);
+    uint64_t *p = reinterpret_cast<uint64_t *>(to);
+    __hip_atomic_store(p, from[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(p + 1, from[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ Term left_term(const Term *from)
+{
+    const uint64_t *p = reinterpret_cast<const uint64_t *>(from);
+    const uint64_t x[2] = {__hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), __hip_atomic_load(p + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)};
+    Term t;
+    __builtin_memcpy(&t, x, sizeof t);
+    return t;
+}
+// by all of a block's threads, behind their rows: the last block's first wavefront adds up the terms of all
+constexpr uint32_t kFewBlocks = 256;
+__device__ __forceinline__ void sum_here(const LossArgs &a)
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_waitcnt(0);               // each wavefront for the term that it has left: the barrier does not wait for stores
+    __syncthreads();
+    if (threadIdx.x >= 64u || !arrives_last(a.counts)) return;
+    Sums s;
+    for (uint32_t i = threadIdx.x; i < a.rows; i += 64u * 4u) {
+        Term t[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) if (i + 64u * k < a.rows) t[k] = left_term(a.terms + i + 64u * k); else t[k].kind = TERM_NONE;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s.add(t[k], a.kl_coef);
+    }
+    s.join();
+    if (threadIdx.x == 0) s.put(a.sums);
+}
+__global__ __launch_bounds__(kBlock) void loss_sums_k(LossArgs a)
+{
+    __shared__ double lds[kWavesPerBlock][kLossSums];
+    Sums s;
+    const uint32_t first = blockIdx.x * kTermBlock, end = a.rows - first < kTermBlock ? a.rows : first + kTermBlock;
+    for (uint32_t i = first + threadIdx.x; i < end; i += kBlock * 4u) {
+        Term t[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) if (i + kBlock * k < end) t[k] = a.terms[i + kBlock * k]; else t[k].kind = TERM_NONE;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s.add(t[k], a.kl_coef);
+    }
+    s.join();
+    if ((threadIdx.x & 63u) == 0)
+#pragma unroll
+        for (int k = 0; k < kLossSums; ++k) lds[threadIdx.x >> 6][k] = s.at[k];
+    __syncthreads();
+    if (threadIdx.x >= 64u) return;
+    double *before = a.partial + (size_t)kLossSums * kLossPartials;
+    const uint32_t k = threadIdx.x;
+    if (k < (uint32_t)kLossSums) leave_sum(a.partial + (size_t)k * kLossPartials + blockIdx.x, (lds[0][k] + lds[1][k]) + (lds[2][k] + lds[3][k]));
+    if (!arrives_last(a.counts) || k >= (uint32_t)kLossSums) return;
+    double sum = a.more ? before[k] : 0.0;
+    for (uint32_t i = 0; i < gridDim.x; ++i) sum += left_sum(a.partial + (size_t)k * kLossPartials + i);
+    before[k] = sum;
+    a.sums[k] = k < 5u ? (float)sum : __int_as_float((int)sum);
+    if (k == 0) a.sums[kLossSums] = 0.0f;
+}
+
+// ---- rows that fit the registers of those who share them ----------------------------------------------------------------
+// 16 bytes of a row, and its elements.
+template <class T> struct Raw;
+template <> struct Raw<float> {
+    static constexpr int N = 4;
+    typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
+    float x[4];
+    __device__ __forceinline__ void none() { for (int e = 0; e < N; ++e) x[e] = kNone; }
+    __device__ __forceinline__ void load(global_ptr<const float> p)
+    {
+        const vec v = __builtin_nontemporal_load((global_ptr<const vec>)p);
+        for (int e = 0; e < N; ++e) x[e] = v[e];
+    }
+    __device__ __forceinline__ float at(int e) const { return x[e]; }
+    __device__ __forceinline__ void forget() { for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(x[e])); }
+};
+// The largest of values seen.
+template <class T> struct Largest;
+template <> struct Largest<float> {
+    float top = kNone;
+    __device__ __forceinline__ void see(const Raw<float> &r) { top = fmaxf(fmaxf(fmaxf(top, r.x[0]), r.x[1]), fmaxf(r.x[2], r.x[3])); }
+    __device__ __forceinline__ float get() const { return top; }
+};
+// Of 16 bits, two to a word.  Read as integers, values from 0 on are in order, and those below 0 in reverse and below all
+// others: the largest signed integer if that is not below 0, else the smallest unsigned one.  That takes two packed
+// instructions for two elements, and no conversion.
+typedef short short2v __attribute__((ext_vector_type(2)));
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+template <class T> struct Raw {
+    static constexpr int N = 8;
+    typedef uint32_t vec __attribute__((ext_vector_type(4), aligned(2)));
+    uint32_t x[4];
+    // what has been computed from the elements so far is not kept for later (it would take twice the registers)
+    __device__ __forceinline__ void forget() { for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(x[e])); }
+    static constexpr uint32_t kNoneBits = std::is_same_v<T, __bf16> ? 0xFF80FF80u : 0xFC00FC00u;
+    __device__ __forceinline__ void none() { for (int e = 0; e < 4; ++e) x[e] = kNoneBits; }
+    __device__ __forceinline__ void load(global_ptr<const T> p)
+    {
+        const vec v = __builtin_nontemporal_load((global_ptr<const vec>)p);
+        for (int e = 0; e < 4; ++e) x[e] = v[e];
+    }
+    __device__ __forceinline__ float at(int e) const
+    {
+        if constexpr (std::is_same_v<T, __bf16>) return __uint_as_float(e & 1 ? x[e >> 1] & 0xFFFF0000u : x[e >> 1] << 16);
+        return (float)__builtin_bit_cast(_Float16, (uint16_t)(e & 1 ? x[e >> 1] >> 16 : x[e >> 1]));
+    }
+};
+template <class T> struct Largest {
+    short2v high = {-32768, -32768};
+    ushort2v low = {65535, 65535};
+    __device__ __forceinline__ void see(const Raw<T> &r)
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            high = __builtin_elementwise_max(high, __builtin_bit_cast(short2v, r.x[e]));
+            low = __builtin_elementwise_min(low, __builtin_bit_cast(ushort2v, r.x[e]));
+        }
+    }
+    __device__ __forceinline__ float get() const
+    {
+        const short h = high[0] > high[1] ? high[0] : high[1];
+        const unsigned short l = low[0] < low[1] ? low[0] : low[1];
+        return (float)__builtin_bit_cast(T, h >= 0 ? (unsigned short)h : l);
+    }
+};
+
+// SHARE threads to a row, each with up to NV 16-byte vectors of it, which are read once, and one element of what is left of the row behind
+// its last whole vector.  KEEP: the exponentials stay in registers between the sum and the gradient, else the logits do.  HERE: the last
+// block adds up the rows' terms.
+template <class T, int SHARE, int NV, bool KEEP, bool LOSS, bool HERE>
+__global__ __launch_bounds__(SHARE < kBlock ? kBlock : SHARE, NV <= 4 ? 8 : 4) void loss_held_k(LossArgs a)
+{
+    constexpr int THREADS = SHARE < kBlock ? kBlock : SHARE, N = Raw<T>::N, WAVES = SHARE / 64;
+    typedef typename VecOf<T, N>::type out_vec;
+    __shared__ float at[2 * WAVES + 1];
+    const uint32_t lane = threadIdx.x % SHARE, vecs = a.vocab / N, rest = a.vocab % N;
+    const uint32_t r = blockIdx.x * (THREADS / SHARE) + __builtin_amdgcn_readfirstlane(threadIdx.x / SHARE);
+    auto body = [&] {
+        const Row row = row_of<LOSS>(a, r);
         const global_ptr<const T> x = in_global(static_cast<const T *>(a.logits)) + (int64_t)r * a.stride;
         const global_ptr<T> dx = in_global(static_cast<T *>(a.dlogits)) + (int64_t)r * a.dstride;
-        if (!taken) {
-            if (LOSS && threadIdx.x == 0 && w != 0.0f) sums[6] += 1.0;
-            if (threadIdx.x == 0 && a.logp) a.logp[r] = 0.0f;
+        auto put = [&](const Term &t) { if (HERE) leave_term(a.terms + r, t); else a.terms[r] = t; };
+        if (!row.taken(a)) {
+            if (lane == 0) {
+                if (LOSS) put({0.0f, 0.0f, row.weight, row.weight != 0.0f ? (uint32_t)TERM_LEFT_OUT : (uint32_t)TERM_NONE});
+                if (a.logp) a.logp[r] = 0.0f;
+            }
+            if (LOSS && a.dlogits) {
+                const out_vec zero = {};
+                for (uint32_t i = lane; i < vecs; i += SHARE) __builtin_nontemporal_store(zero, (global_ptr<out_vec>)(dx + (size_t)i * N));
+                if (lane < rest) dx[vecs * N + lane] = (T)0.0f;
+            }
+            return;
+        }
+        Raw<T> raw[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const uint32_t i = (uint32_t)k * SHARE + lane;
+            if (i < vecs) raw[k].load(x + (size_t)i * N); else raw[k].none();
+        }
+        const float last = lane < rest ? (float)x[vecs * N + lane] : kNone;
+        float xa = (float)x[row.label];
+        Largest<T> seen;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) seen.see(raw[k]);
+        const float wtop = wave_max(fmaxf(seen.get(), last)), wbase = base_of(wtop);
+        if (sizeof(T) < 4)
+#pragma unroll
+            for (int k = 0; k < NV; ++k) raw[k].forget();
+        float e[KEEP ? NV * N : 1], sum = row_exp<T>(a, last, wbase);
+        const float elast = sum;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float y = row_exp<T>(a, raw[k].at(j), wbase);
+                if (KEEP) e[k * N + j] = y;
+                sum += y;
+            }
+        sum = wave_sum_f(sum);
+        // The wavefronts' maxima and sums, and the label's logit as the first
+        // wavefront has read it: where the gradient takes the logits' place, another one may have overwritten it behind the barrier.
+        float top = wbase, part = 1.0f;
+        if constexpr (WAVES > 1) {
+            if ((threadIdx.x & 63u) == 0) { at[lane >> 6] = wtop; at[WAVES + (lane >> 6)] = sum; }
+            if (lane == 0) at[2 * WAVES] = xa;
+            __syncthreads();
+            xa = at[2 * WAVES];
+            const float m = at[lane % WAVES];
+            top = m;
+#pragma unroll
+            for (int w = WAVES / 2; w >= 1; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, 64));
+            top = base_of(top);
+            sum = at[WAVES + lane % WAVES] * row_exp<T>(a, m, top);
+#pragma unroll
+            for (int w = WAVES / 2; w >= 1; w >>= 1) sum += __shfl_xor(sum, w, 64);
+            part = row_exp<T>(a, wtop, top);
+        }
+        const double l = ((double)xa - (double)top) * a.inv_t - log_wide(sum);
+        if (lane == 0 && a.logp) a.logp[r] = (float)l;
+        if (!LOSS) return;
+        const RowTerms t = row_terms(a, r, l);
+        if (lane == 0) put({t.policy, t.kl, row.weight, t.cut ? (uint32_t)TERM_CUT : (uint32_t)TERM_FREE});
+        if (!a.dlogits) return;
+        const float slope = row.weight * t.slope * a.gscale;
+        part *= -slope / sum;
+        if (!KEEP)
+#pragma unroll
+            for (int k = 0; k < NV; ++k) raw[k].forget();
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const uint32_t i = (uint32_t)k * SHARE + lane;
+            out_vec v;
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = (T)(part * (KEEP ? e[k * N + j] : row_exp<T>(a, raw[k].at(j), wbase)));
+            if (i < vecs) __builtin_nontemporal_store(v, (global_ptr<out_vec>)(dx + (size_t)i * N));
+        }
+        if (lane < rest) dx[vecs * N + lane] = (T)(part * elast);
+        // the label's own element, by the thread that has stored it with the others
+        const uint32_t label = (uint32_t)row.label;
+        if (lane == (label < vecs * N ? label / N % SHARE : label - vecs * N)) dx[label] = (T)(part * row_exp<T>(a, xa, wbase) + slope);
+    };
+    if (r < a.rows) body();
+    if (HERE) sum_here(a);
+}
+
+// ---- longer rows --------------------------------------------------------------------------------------------------------------
+// One block to a row, two passes over it: the running maximum and sum, then the gradient.
+template <class T, bool LOSS, bool HERE>
+__global__ __launch_bounds__(kBlock) void loss_long_k(LossArgs a)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    __shared__ float lds[2 * kWavesPerBlock + 1];
+    const uint32_t r = blockIdx.x;
+    auto body = [&] {
+        const Row row = row_of<LOSS>(a, r);
+        const global_ptr<const T> x = in_global(static_cast<const T *>(a.logits)) + (int64_t)r * a.stride;
+        const global_ptr<T> dx = in_global(static_cast<T *>(a.dlogits)) + (int64_t)r * a.dstride;
+        auto put = [&](const Term &t) { if (HERE) leave_term(a.terms + r, t); else a.terms[r] = t; };
+        if (!row.taken(a)) {
+            if (threadIdx.x == 0) {
+                if (LOSS) put({0.0f, 0.0f, row.weight, row.weight != 0.0f ? (uint32_t)TERM_LEFT_OUT : (uint32_t)TERM_NONE});
+                if (a.logp) a.logp[r] = 0.0f;
+            }
             if (LOSS && a.dlogits) {
                 const float zero[N] = {};
                 for (uint32_t i = threadIdx.x * N; i < a.vocab; i += kBlock * N) store_some<N, T>(dx, i, a.vocab, zero);
             }
-            continue;
+            return;
         }
-        const float xa = (float)x[label];
-        float top = -__builtin_inff(), sum = 0.0f;
+        float xa = (float)x[row.label], top = kNone, sum = 0.0f;
         for (uint32_t i = threadIdx.x * N; i < a.vocab; i += kBlock * N) {
             float v[N], most;
-            load_some<N, T>(x, i, a.vocab, v, -__builtin_inff());
+            load_some<N, T>(x, i, a.vocab, v, kNone);
             most = v[0];
 #pragma unroll
             for (int e = 1; e < N; ++e) most = fmaxf(most, v[e]);
@@ -72,11 +367,11 @@ __global__ __launch_bounds__(kBlock) void loss_rows_k(LossArgs a)
             for (int e = 0; e < N; ++e) sum += row_exp<T>(a, v[e], base);
         }
         const float wtop = wave_max(top);
-        sum *= row_exp<T>(a, top, base_of(wtop));
-#pragma unroll
-        for (int m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m, 64);
+        sum = wave_sum_f(sum * row_exp<T>(a, top, base_of(wtop)));
         if ((threadIdx.x & 63u) == 0) { lds[threadIdx.x >> 6] = wtop; lds[kWavesPerBlock + (threadIdx.x >> 6)] = sum; }
+        if (threadIdx.x == 0) lds[2 * kWavesPerBlock] = xa;      // (see above)
         __syncthreads();
+        xa = lds[2 * kWavesPerBlock];
         top = lds[0];
 #pragma unroll
         for (int k = 1; k < kWavesPerBlock; ++k) top = fmaxf(top, lds[k]);
@@ -85,59 +380,85 @@ __global__ __launch_bounds__(kBlock) void loss_rows_k(LossArgs a)
 #pragma unroll
         for (int k = 0; k < kWavesPerBlock; ++k) sum += lds[kWavesPerBlock + k] * row_exp<T>(a, lds[k], top);
         __syncthreads();
-        const float logp = (xa - top) * a.inv_t - logf(sum);
-        if (threadIdx.x == 0 && a.logp) a.logp[r] = logp;
-        if (!LOSS) continue;
-        const RowTerms t = row_terms(a, r, logp);
-        if (threadIdx.x == 0) {
-            const double wd = w;
-            sums[0] += wd * ((double)t.policy + (double)a.kl_coef * t.kl);
-            sums[1] += wd * t.policy; sums[2] += wd * t.kl; sums[3] += wd * t.cut; sums[4] += wd; sums[5] += 1.0;
-        }
-        if (!a.dlogits) continue;
-        const float slope = w * t.slope * a.gscale, part = -slope / sum;
+        const double l = ((double)xa - (double)top) * a.inv_t - log_wide(sum);
+        if (threadIdx.x == 0 && a.logp) a.logp[r] = (float)l;
+        if (!LOSS) return;
+        const RowTerms t = row_terms(a, r, l);
+        if (threadIdx.x == 0) put({t.policy, t.kl, row.weight, t.cut ? (uint32_t)TERM_CUT : (uint32_t)TERM_FREE});
+        if (!a.dlogits) return;
+        const float slope = row.weight * t.slope * a.gscale, part = -slope / sum;
         for (uint32_t i = threadIdx.x * N; i < a.vocab; i += kBlock * N) {
             float v[N];
-            load_some<N, T>(x, i, a.vocab, v, -__builtin_inff());
+            load_some<N, T>(x, i, a.vocab, v, kNone);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 v[e] = part * row_exp<T>(a, v[e], top);
-                if (i + (uint32_t)e == (uint32_t)label) v[e] += slope;
+                if (i + (uint32_t)e == (uint32_t)row.label) v[e] += slope;
             }
             store_some<N, T>(dx, i, a.vocab, v);
         }
-    }
-    if (LOSS && threadIdx.x == 0)
-#pragma unroll
-        for (int k = 0; k < kLossSums; ++k) a.partial[(size_t)blockIdx.x * kLossSums + k] = sums[k];
+    };
+    body();
+    if (HERE) sum_here(a);
 }
 
-__global__ __launch_bounds__(kBlock) void loss_finish_k(const double *partial, uint32_t count, float *out)
+// ---- launches -----------------------------------------------------------------------------------------------------------------
+template <class T, int SHARE, int NV, bool KEEP, bool LOSS>
+static bool held(const LaunchCtx &lc, const LossArgs &a)
 {
-    __shared__ double lds[kWavesPerBlock];
-    for (int k = 0; k < kLossSums; ++k) {
-        double sum = 0.0;
-        for (uint32_t i = threadIdx.x; i < count; i += kBlock) sum += partial[(size_t)i * kLossSums + k];
-        sum = block_sum(sum, lds);
-        if (threadIdx.x == 0) out[k] = k < 5 ? (float)sum : __int_as_float((int)sum);
-    }
-    if (threadIdx.x == 0) out[7] = 0.0f;
+    constexpr uint32_t THREADS = SHARE < kBlock ? kBlock : SHARE, each = THREADS / SHARE;
+    const uint32_t blocks = (a.rows + each - 1) / each;
+    const bool here = LOSS && blocks <= kFewBlocks && !a.more;
+    launch(here ? loss_held_k<T, SHARE, NV, KEEP, LOSS, LOSS> : loss_held_k<T, SHARE, NV, KEEP, LOSS, false>, dim3(blocks), dim3(THREADS), lc.stream, a);
+    return here;
 }
+// At most kTermRows rows; whether their terms are added up.
+template <class T, bool LOSS>
+static bool loss_of(const LaunchCtx &lc, const LossArgs &a)
+{
+    const uint32_t vecs = a.vocab / Raw<T>::N;
+    if (vecs <= 64 * 1) return held<T, 64, 1, true, LOSS>(lc, a);
+    if (vecs <= 64 * 2) return held<T, 64, 2, true, LOSS>(lc, a);
+    if (vecs <= 64 * 4) return held<T, 64, 4, true, LOSS>(lc, a);
+    if (vecs <= 256 * 2) return held<T, 256, 2, true, LOSS>(lc, a);
+    if (vecs <= 256 * 4) return held<T, 256, 4, true, LOSS>(lc, a);
+    if (vecs <= 1024 * 2) return held<T, 1024, 2, true, LOSS>(lc, a);
+    if (vecs <= 1024 * 4) return held<T, 1024, 4, true, LOSS>(lc, a);
+    if (vecs <= 1024 * 8) return held<T, 1024, 8, false, LOSS>(lc, a);
+    if (vecs <= 1024 * 16) return held<T, 1024, 16, false, LOSS>(lc, a);
+    const bool here = LOSS && a.rows <= kFewBlocks && !a.more;
+    launch(here ? loss_long_k<T, LOSS, LOSS> : loss_long_k<T, LOSS, false>, dim3(a.rows), dim3(kBlock), lc.stream, a);
+    return here;
+}
+// the sums of no rows
+__global__ void no_rows_k(float *sums) { if (threadIdx.x <= (uint32_t)kLossSums) sums[threadIdx.x] = 0.0f; }
 
-template <class T>
-static void loss_of(const LaunchCtx &lc, const LossArgs &a, bool loss)
+template <bool LOSS>
+static void loss_by(const LaunchCtx &lc, int dtype, LossArgs a)
 {
-    const uint32_t blocks = a.rows < kLossBlocks ? a.rows : kLossBlocks;
-    if (blocks) launch(loss ? loss_rows_k<T, true> : loss_rows_k<T, false>, dim3(blocks), dim3(kBlock), lc.stream, a);
-    if (loss) launch(loss_finish_k, dim3(1), dim3(kBlock), lc.stream, a.partial, blocks, a.sums);
+    const uintptr_t size = dtype == MC_DTYPE_F32 ? 4u : 2u;
+    for (uint32_t left = a.rows; left;) {
+        a.rows = left < kTermRows ? left : kTermRows;
+        const bool done = dtype == MC_DTYPE_F32 ? loss_of<float, LOSS>(lc, a) : dtype == MC_DTYPE_BF16 ? loss_of<__bf16, LOSS>(lc, a) : loss_of<_Float16, LOSS>(lc, a);
+        if (LOSS && !done) launch(loss_sums_k, dim3((a.rows + kTermBlock - 1) / kTermBlock), dim3(kBlock), lc.stream, a);
+        left -= a.rows;
+        a.more = true;
+        a.logits = static_cast<const char *>(a.logits) + (int64_t)a.rows * a.stride * size;
+        if (a.dlogits) a.dlogits = static_cast<char *>(a.dlogits) + (int64_t)a.rows * a.dstride * size;
+        a.labels += a.rows;
+        if (a.logp) a.logp += a.rows;
+        if (!LOSS) continue;
+        a.old_logp += a.rows;
+        a.advantages += a.rows;
+        if (a.weights) a.weights += a.rows;
+        if (a.ref_logp) a.ref_logp += a.rows;
+    }
 }
-static void loss_by(const LaunchCtx &lc, int dtype, const LossArgs &a, bool loss)
+void launch_token_logp(const LaunchCtx &lc, int dtype, const LossArgs &a) { loss_by<false>(lc, dtype, a); }
+void launch_policy_loss(const LaunchCtx &lc, int dtype, const LossArgs &a)
 {
-    if (dtype == MC_DTYPE_F32) loss_of<float>(lc, a, loss);
-    else if (dtype == MC_DTYPE_BF16) loss_of<__bf16>(lc, a, loss);
-    else loss_of<_Float16>(lc, a, loss);
+    if (a.rows) loss_by<true>(lc, dtype, a);
+    else launch(no_rows_k, dim3(1), dim3(64), lc.stream, a.sums);
 }
-void launch_token_logp(const LaunchCtx &lc, int dtype, const LossArgs &a) { loss_by(lc, dtype, a, false); }
-void launch_policy_loss(const LaunchCtx &lc, int dtype, const LossArgs &a) { loss_by(lc, dtype, a, true); }
 
 }  // namespace mc

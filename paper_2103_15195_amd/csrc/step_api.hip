@@ -21,7 +21,9 @@ struct mc_step {
 };
 struct mc_loss {
     int device = 0;
+    Term *d_terms = nullptr;
     double *d_partial = nullptr;
+    uint32_t *d_counts = nullptr;        // 0 between calls
 };
 
 namespace {
@@ -182,7 +184,9 @@ int mc_loss_destroy(mc_loss *h)
     {
         OnDevice guard(h->device);
         (void)hipDeviceSynchronize();
+        if (h->d_terms) (void)hipFree(h->d_terms);
         if (h->d_partial) (void)hipFree(h->d_partial);
+        if (h->d_counts) (void)hipFree(h->d_counts);
     }
     delete h;
     return MC_OK;
@@ -195,7 +199,11 @@ int mc_loss_create(mc_loss **out)
     mc_loss *h = new (std::nothrow) mc_loss();
     if (!h) return MC_ERR_ALLOC;
     if (hipGetDevice(&h->device) != hipSuccess) { (void)hipGetLastError(); delete h; return MC_ERR_DEVICE; }
-    const int rc = grab(&h->d_partial, (size_t)kLossBlocks * kLossSums * sizeof(double));
+    int rc = grab(&h->d_partial, (size_t)(kLossPartials + 1) * kLossSums * sizeof(double));
+    if (rc == MC_OK) rc = grab(&h->d_terms, (size_t)kTermRows * sizeof(Term));
+    if (rc == MC_OK) rc = grab(&h->d_counts, kArriveBytes);
+    if (rc == MC_OK && hipMemset(h->d_counts, 0, kArriveBytes) != hipSuccess) rc = MC_ERR_DEVICE;
+    if (rc == MC_OK && hipDeviceSynchronize() != hipSuccess) rc = MC_ERR_DEVICE;      // (before work on any stream)
     if (rc != MC_OK) { mc_loss_destroy(h); return rc; }
     *out = h;
     return MC_OK;
@@ -217,8 +225,10 @@ static int logits_args(const mc_loss *h, const mc_logits *x, LossArgs &a)
     const double base2 = 1.4426950408889634 / (double)x->temperature;
     a.to_base2 = (float)base2;
     a.to_base2_rest = (float)(base2 - (double)a.to_base2);
-    a.inv_t = (float)(1.0 / (double)x->temperature);
+    a.inv_t = 1.0 / (double)x->temperature;
     a.partial = h->d_partial;
+    a.terms = h->d_terms;
+    a.counts = h->d_counts;
     return MC_OK;
 }
 

@@ -39,7 +39,15 @@ void launch_adamw(const LaunchCtx &lc, int dtype, int model_dtype, const StepVie
 
 // ---- rows of logits -----------------------------------------------------------------------------------------------
 constexpr int kLossSums = 7;                 // five sums and two counts
-constexpr uint32_t kLossBlocks = 2048;
+// What a row adds to them.
+struct alignas(16) Term {
+    float policy, kl, weight;
+    uint32_t kind;
+};
+enum TermKind { TERM_NONE = 0, TERM_FREE = 1, TERM_CUT = 2, TERM_LEFT_OUT = 3 };      // takes no part; does; does and the clamp decides; has a weight, but no valid label
+constexpr uint32_t kTermRows = 1u << 17;     // rows that there is room for: more of them are taken so many at a time
+constexpr uint32_t kTermBlock = 4096;        // rows per block of the kernel that adds them up
+constexpr uint32_t kLossPartials = kTermRows / kTermBlock;
 struct LossArgs {
     const void *logits;
     const int64_t *labels;
@@ -49,11 +57,47 @@ struct LossArgs {
     int64_t stride, dstride;
     uint32_t rows, vocab;
     float to_base2, to_base2_rest;           // log2(e) / temperature, in two parts
-    float inv_t, lo, hi, kl_coef, gscale;    // gscale: grad_scale / temperature
-    double *partial;
+    double inv_t;
+    float lo, hi, kl_coef, gscale;           // gscale: grad_scale / temperature
+    Term *terms;                             // kTermRows
+    double *partial;                         // kLossSums lists of kLossPartials sums, then the sums of the rows before these
+    uint32_t *counts;                        // kArriveBytes
+    bool more;                               // there are rows before these
 };
 void launch_token_logp(const LaunchCtx &lc, int dtype, const LossArgs &a);
 void launch_policy_loss(const LaunchCtx &lc, int dtype, const LossArgs &a);
+
+// ---- sums over all blocks of a launch -----------------------------------------------------------------------------
+// Every block leaves its sums and adds one to a count; the block that finds all others' additions there combines them, in an order that
+// does not depend on which block that is.  Additions to one line take 30 ns each where the blocks sit on different dies: up to
+// kArriveFlat blocks share one count, more of them are counted in kArriveGroups groups, each on a line of its own, whose last
+// blocks are counted in turn.  All counts are 0 again when the launch is over.
+constexpr uint32_t kArriveFlat = 48, kArriveGroups = 32, kArriveLine = 32;           // (words between counts)
+constexpr size_t kArriveBytes = (kArriveGroups + 1) * kArriveLine * sizeof(uint32_t);
+__device__ __forceinline__ void leave_sum(double *p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ double left_sum(const double *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// One wavefront, whose lanes have left the block's sums: whether this is the last block.
+__device__ __forceinline__ bool arrives_last(uint32_t *counts)
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_waitcnt(0);               // the sums are written through before a count says so
+    uint32_t last = 0;
+    if ((threadIdx.x & 63u) == 0) {
+        const uint32_t blocks = gridDim.x, groups = blocks <= kArriveFlat ? 1u : kArriveGroups, g = blockIdx.x % groups;
+        const uint32_t members = (blocks - g + groups - 1u) / groups;
+        uint32_t *mine = counts + (1u + g) * kArriveLine;
+        last = __hip_atomic_fetch_add(mine, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == members - 1u;
+        if (last) {
+            __hip_atomic_store(mine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (groups > 1u) {
+                last = __hip_atomic_fetch_add(counts, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == groups - 1u;
+                if (last) __hip_atomic_store(counts, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");       // (the sums are read past the caches, but not before the count)
+    return __builtin_amdgcn_readfirstlane((int)last) != 0;
+}
 
 // ---- values of 32 and 16 bits ---------------------------------------------------------------------------------------
 template <class T, int N> struct VecOf;
