@@ -350,14 +350,14 @@ __global__ __launch_bounds__(kBlock) void loss_long_k(LossArgs a)
             }
             if (LOSS && a.dlogits) {
                 const float zero[N] = {};
-                for (uint32_t i = threadIdx.x * N; i < a.vocab; i += kBlock * N) store_some<N, T>(dx, i, a.vocab, zero);
+                for (uint32_t i = threadIdx.x * N; i < a.vocab; i += kBlock * N) store_some<N, T>(dx, (int32_t)i, 0, (int32_t)a.vocab, zero);
             }
             return;
         }
         float xa = (float)x[row.label], top = kNone, sum = 0.0f;
         for (uint32_t i = threadIdx.x * N; i < a.vocab; i += kBlock * N) {
             float v[N], most;
-            load_some<N, T>(x, i, a.vocab, v, kNone);
+            load_some<N, T>(x, (int32_t)i, 0, (int32_t)a.vocab, v, kNone);
             most = v[0];
 #pragma unroll
             for (int e = 1; e < N; ++e) most = fmaxf(most, v[e]);
@@ -389,13 +389,13 @@ __global__ __launch_bounds__(kBlock) void loss_long_k(LossArgs a)
         const float slope = row.weight * t.slope * a.gscale, part = -slope / sum;
         for (uint32_t i = threadIdx.x * N; i < a.vocab; i += kBlock * N) {
             float v[N];
-            load_some<N, T>(x, i, a.vocab, v, kNone);
+            load_some<N, T>(x, (int32_t)i, 0, (int32_t)a.vocab, v, kNone);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 v[e] = part * row_exp<T>(a, v[e], top);
                 if (i + (uint32_t)e == (uint32_t)row.label) v[e] += slope;
             }
-            store_some<N, T>(dx, i, a.vocab, v);
+            store_some<N, T>(dx, (int32_t)i, 0, (int32_t)a.vocab, v);
         }
     };
     body();

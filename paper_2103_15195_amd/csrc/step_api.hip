@@ -16,6 +16,7 @@ struct mc_step {
     Piece *d_pieces = nullptr;
     uintptr_t *d_addr = nullptr;         // MC_LISTS lists of the live tensors' addresses
     double *d_partial = nullptr;
+    uint32_t *d_counts = nullptr;        // 0 between calls
     std::vector<uintptr_t> want;         // a list on its way to the device (reserved at creation)
     bool bound[MC_LISTS] = {};
 };
@@ -59,6 +60,14 @@ int grab(T **p, size_t bytes)
     return MC_OK;
 }
 
+int grab_counts(uint32_t **p)
+{
+    const int rc = grab(p, kArriveBytes);
+    if (rc != MC_OK) return rc;
+    // (done before work on any stream)
+    return hipMemset(*p, 0, kArriveBytes) == hipSuccess && hipDeviceSynchronize() == hipSuccess ? MC_OK : MC_ERR_DEVICE;
+}
+
 }  // namespace
 
 extern "C" {
@@ -72,6 +81,7 @@ int mc_step_destroy(mc_step *h)
         if (h->d_pieces) (void)hipFree(h->d_pieces);
         if (h->d_addr) (void)hipFree(h->d_addr);
         if (h->d_partial) (void)hipFree(h->d_partial);
+        if (h->d_counts) (void)hipFree(h->d_counts);
     }
     delete h;
     return MC_OK;
@@ -87,7 +97,7 @@ int mc_step_create(mc_step **out, const int64_t *numel, int32_t n_tensors, int32
     for (int32_t t = 0; t < n_tensors; ++t) {
         if (numel[t] < 0) return MC_ERR_INVALID_ARG;
         if (numel[t] >= (int64_t(1) << 43)) return MC_ERR_RANGE;
-        pieces += ((uint64_t)numel[t] + kPiece - 1) / kPiece;
+        pieces += numel[t] ? ((uint64_t)numel[t] + kMostShift + kPiece - 1) / kPiece : 0;
         if (pieces >= (uint64_t(1) << 31)) return MC_ERR_RANGE;
     }
     mc_step *h = new (std::nothrow) mc_step();
@@ -105,11 +115,12 @@ int mc_step_create(mc_step **out, const int64_t *numel, int32_t n_tensors, int32
             if (numel[t] == 0) continue;
             const uint32_t name = (uint32_t)h->live.size() | (no_decay && no_decay[t] ? kNoDecay : 0u);
             h->live.push_back(t);
-            for (int64_t at = 0, i = 0; at < numel[t]; at += kPiece, ++i)
-                table.push_back({name, (uint32_t)i, (uint32_t)(numel[t] - at < (int64_t)kPiece ? numel[t] - at : kPiece), 0u});
+            for (int64_t at = 0, i = 0; at < numel[t] + (int64_t)kMostShift; at += kPiece, ++i)
+                table.push_back({name, (uint32_t)i, (int32_t)(numel[t] - at < (int64_t)kPiece ? numel[t] - at : kPiece), 0u});
         }
         h->want.reserve(h->live.size());
-        if (rc == MC_OK) rc = grab(&h->d_partial, kNormBlocks * sizeof(double));
+        rc = grab(&h->d_partial, kNormBlocks * sizeof(double));
+        if (rc == MC_OK) rc = grab_counts(&h->d_counts);
         if (rc == MC_OK && pieces) rc = grab(&h->d_pieces, table.size() * sizeof(Piece));
         if (rc == MC_OK && pieces) rc = grab(&h->d_addr, (size_t)MC_LISTS * h->live.size() * sizeof(uintptr_t));
         if (rc == MC_OK && pieces && hipMemcpy(h->d_pieces, table.data(), table.size() * sizeof(Piece), hipMemcpyHostToDevice) != hipSuccess) rc = MC_ERR_DEVICE;
@@ -145,7 +156,7 @@ int mc_grad_norm(mc_step *h, float scale, float max_norm, float *out, void *stre
 {
     const int rc = norm_args(h, scale, max_norm, out);
     if (rc != MC_OK) return rc;
-    launch_grad_norm(on(stream), h->grad_dtype, view(h), h->d_partial, scale, max_norm, out);
+    launch_grad_norm(on(stream), h->grad_dtype, view(h), h->d_partial, h->d_counts, scale, max_norm, out);
     return launched();
 }
 
@@ -154,7 +165,7 @@ int mc_grad_clip(mc_step *h, float scale, float max_norm, float *out, void *stre
     const int rc = norm_args(h, scale, max_norm, out);
     if (rc != MC_OK) return rc;
     const LaunchCtx lc = on(stream);
-    launch_grad_norm(lc, h->grad_dtype, view(h), h->d_partial, scale, max_norm, out);
+    launch_grad_norm(lc, h->grad_dtype, view(h), h->d_partial, h->d_counts, scale, max_norm, out);
     launch_grad_clip(lc, h->grad_dtype, view(h), h->bound[MC_LIST_CLIPPED] ? MC_LIST_CLIPPED : MC_LIST_GRADS, out + 1);
     return launched();
 }
@@ -201,9 +212,7 @@ int mc_loss_create(mc_loss **out)
     if (hipGetDevice(&h->device) != hipSuccess) { (void)hipGetLastError(); delete h; return MC_ERR_DEVICE; }
     int rc = grab(&h->d_partial, (size_t)(kLossPartials + 1) * kLossSums * sizeof(double));
     if (rc == MC_OK) rc = grab(&h->d_terms, (size_t)kTermRows * sizeof(Term));
-    if (rc == MC_OK) rc = grab(&h->d_counts, kArriveBytes);
-    if (rc == MC_OK && hipMemset(h->d_counts, 0, kArriveBytes) != hipSuccess) rc = MC_ERR_DEVICE;
-    if (rc == MC_OK && hipDeviceSynchronize() != hipSuccess) rc = MC_ERR_DEVICE;      // (before work on any stream)
+    if (rc == MC_OK) rc = grab_counts(&h->d_counts);
     if (rc != MC_OK) { mc_loss_destroy(h); return rc; }
     *out = h;
     return MC_OK;

@@ -6,13 +6,15 @@
 namespace mc {
 
 // ---- lists of tensors ---------------------------------------------------------------------------------------------
-// Work is handed out in pieces of at most kPiece consecutive elements of one tensor.
-constexpr uint32_t kPiece = 4096;
+// Work is handed out in pieces of kPiece elements of a tensor, counted from the 128-byte line that the tensor begins in (in the list
+// that a kernel writes): every piece but the first then begins on a line, wherever the tensors lie, and a piece more than
+// the elements need stands ready for those that the beginning takes.
+constexpr uint32_t kPiece = 4096, kLine = 128, kMostShift = kLine / 2 - 1;       // (elements of 16 bits)
 constexpr uint32_t kNoDecay = 0x80000000u;
 struct alignas(16) Piece {
     uint32_t tensor;             // its place in the lists of addresses; kNoDecay: not decayed
-    uint32_t index;              // the piece begins at element kPiece * index of it
-    uint32_t count;
+    uint32_t index;              // which of the tensor's pieces
+    int32_t left;                // elements from kPiece * index on, if that many are within reach (below 0: the one more)
     uint32_t pad;
 };
 // A handle's lists as the kernels see them: the addresses of list l are addr[l * tensors ..].
@@ -22,7 +24,7 @@ struct StepView {
     uint32_t npieces, tensors;
 };
 // blocks of the norm's first pass, at most, and the scratch that they leave their sums in
-constexpr uint32_t kNormBlocks = 2048;
+constexpr uint32_t kNormBlocks = 1024;
 
 struct AdamwArgs {
     const float *coef;           // null: 1
@@ -33,7 +35,8 @@ struct AdamwArgs {
     float eps;
 };
 
-void launch_grad_norm(const LaunchCtx &lc, int dtype, const StepView &v, double *partial, float scale, float max_norm, float *out);
+void launch_grad_norm(const LaunchCtx &lc, int dtype, const StepView &v, double *partial, uint32_t *counts, float scale, float max_norm,
+                      float *out);
 void launch_grad_clip(const LaunchCtx &lc, int dtype, const StepView &v, uint32_t to_list, const float *coef);
 void launch_adamw(const LaunchCtx &lc, int dtype, int model_dtype, const StepView &v, const AdamwArgs &a);
 
@@ -109,32 +112,33 @@ MC_VEC(_Float16, 4, 2);
 MC_VEC(_Float16, 8, 2);
 #undef MC_VEC
 
-// N consecutive elements from p + i, those from `count` on as `fill`
-template <int N, class T>
-__device__ __forceinline__ void load_some(global_ptr<const T> p, uint32_t i, uint32_t count, float (&v)[N], float fill = 0.0f)
+// N consecutive elements from p + i, of those from `lo` to `hi` (the others: `fill`).  STREAM: not to be kept in the caches.
+template <int N, class T, bool STREAM = true>
+__device__ __forceinline__ void load_some(global_ptr<const T> p, int32_t i, int32_t lo, int32_t hi, float (&v)[N], float fill = 0.0f)
 {
     typedef typename VecOf<T, N>::type vec;
-    if (i + (uint32_t)N <= count) {
-        const vec x = __builtin_nontemporal_load((global_ptr<const vec>)(p + i));
+    if (i >= lo && i + N <= hi) {
+        const global_ptr<const vec> q = (global_ptr<const vec>)(p + i);
+        const vec x = STREAM ? __builtin_nontemporal_load(q) : *q;
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = (float)x[e];
     } else {
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = i + (uint32_t)e < count ? (float)p[i + e] : fill;
+        for (int e = 0; e < N; ++e) v[e] = i + e >= lo && i + e < hi ? (float)p[i + e] : fill;
     }
 }
 template <int N, class T>
-__device__ __forceinline__ void store_some(global_ptr<T> p, uint32_t i, uint32_t count, const float (&v)[N])
+__device__ __forceinline__ void store_some(global_ptr<T> p, int32_t i, int32_t lo, int32_t hi, const float (&v)[N])
 {
     typedef typename VecOf<T, N>::type vec;
-    if (i + (uint32_t)N <= count) {
+    if (i >= lo && i + N <= hi) {
         vec x;
 #pragma unroll
         for (int e = 0; e < N; ++e) x[e] = (T)v[e];
         __builtin_nontemporal_store(x, (global_ptr<vec>)(p + i));
     } else {
 #pragma unroll
-        for (int e = 0; e < N; ++e) if (i + (uint32_t)e < count) p[i + e] = (T)v[e];
+        for (int e = 0; e < N; ++e) if (i + e >= lo && i + e < hi) p[i + e] = (T)v[e];
     }
 }
 
