@@ -14,9 +14,9 @@
  *   - those of mergecomp.h: pointers are "host" or "device" as stated, calls only enqueue kernels on the caller's stream
  *     (void* = hipStream_t), allocate nothing, never synchronise and read nothing back; all calls on one handle must be
  *     issued in stream order, since its scratch is shared between them.  0 or a negative mc_status; no call throws or aborts.
- *   - Arithmetic is binary32, sums over more than a row's share of one thread in binary64 in an order that depends on sizes and device alone:
- *     the same inputs give the same bits.  Values of 16 bits are widened when they are read and rounded once, to nearest
- *     even, when they are written.
+ *   - Arithmetic is binary32; sums over tensors and over rows are binary64.  Sums are taken in an order that depends on sizes, on where
+ *     rows and tensors begin in a cache line, and on the device alone: the same call gives the same bits.  Values of 16
+ *     bits are widened when they are read and rounded once, to nearest even, when they are written.
  *   - Tensors may start at any address that is a multiple of their element size; multiples of 16 bytes are fastest.
  */
 #ifndef MERGECOMP_STEP_H

@@ -33,28 +33,39 @@ __device__ __forceinline__ float wave_sum_f(float x)
     return x;
 }
 
-// What a row is besides its logits.  A row's number is the same for a wavefront, and what is looked up by it comes through the scalar
-// cache and stays in scalar registers.
+// What a row is besides its logits, all asked for at once.  Where a wavefront has one row, this comes through the scalar cache and stays in scalar
+// registers.
 struct Row {
     int64_t label;
-    float weight;
+    float weight, adv, old, ref;
     __device__ __forceinline__ bool valid(const LossArgs &a) const { return label >= 0 && label < (int64_t)a.vocab; }
     __device__ __forceinline__ bool taken(const LossArgs &a) const { return valid(a) && weight != 0.0f; }
 };
-template <bool LOSS>
+template <bool ONE, class T>
+__device__ __forceinline__ T of_row(const T *p, uint32_t r)
+{
+    if constexpr (ONE) return ld_uniform(p + r);
+    return in_global(p)[r];
+}
+template <bool LOSS, bool ONE>
 __device__ __forceinline__ Row row_of(const LossArgs &a, uint32_t r)
 {
-    Row row{ld_uniform(a.labels + r), 1.0f};
-    if (LOSS && a.weights) row.weight = ld_uniform(a.weights + r);
+    Row row{of_row<ONE>(a.labels, r), 1.0f, 0.0f, 0.0f, 0.0f};
+    if (LOSS) {
+        row.adv = of_row<ONE>(a.advantages, r);
+        row.old = of_row<ONE>(a.old_logp, r);
+        if (a.weights) row.weight = of_row<ONE>(a.weights, r);
+        if (a.ref_logp) row.ref = of_row<ONE>(a.ref_logp, r);
+    }
     return row;
 }
 
 // What a row adds to the sums, and the slope of its loss by its log-probability l.
 struct RowTerms { float policy, kl, slope; bool cut; };
-__device__ __forceinline__ RowTerms row_terms(const LossArgs &a, uint32_t r, double l)
+__device__ __forceinline__ RowTerms row_terms(const LossArgs &a, const Row &row, double l)
 {
     RowTerms t;
-    const float adv = ld_uniform(a.advantages + r), rho = expf((float)(l - (double)ld_uniform(a.old_logp + r)));
+    const float adv = row.adv, rho = expf((float)(l - (double)row.old));
     const float free = -adv * rho, held = -adv * fminf(fmaxf(rho, a.lo), a.hi);
     const bool is_free = !(free < held);              // (NaN: the ratio's)
     t.policy = is_free ? free : held;
@@ -62,7 +73,7 @@ __device__ __forceinline__ RowTerms row_terms(const LossArgs &a, uint32_t r, dou
     t.cut = !is_free;
     t.kl = 0.0f;
     if (a.ref_logp) {
-        const float d = (float)((double)ld_uniform(a.ref_logp + r) - l), ed = expf(d);
+        const float d = (float)((double)row.ref - l), ed = expf(d);
         t.kl = ed - d - 1.0f;
         t.slope += a.kl_coef * (1.0f - ed);
     }
@@ -230,51 +241,100 @@ template <class T> struct Largest {
     }
 };
 
-// SHARE threads to a row, each with up to NV 16-byte vectors of it, which are read once, and one element of what is left of the row behind
-// its last whole vector.  KEEP: the exponentials stay in registers between the sum and the gradient, else the logits do.  HERE: the last
-// block adds up the rows' terms.
+// Over the SHARE (or, of more than a wavefront, 64) lanes that share a row.
+template <int SHARE>
+__device__ __forceinline__ float share_max(float x)
+{
+#pragma unroll
+    for (int m = (SHARE < 64 ? SHARE : 64) / 2; m >= 1; m >>= 1) x = fmaxf(x, __shfl_xor(x, m, 64));
+    return x;
+}
+template <int SHARE>
+__device__ __forceinline__ float share_sum(float x)
+{
+#pragma unroll
+    for (int m = (SHARE < 64 ? SHARE : 64) / 2; m >= 1; m >>= 1) x += __shfl_xor(x, m, 64);
+    return x;
+}
+
+// Where a row's vectors lie.  They are counted from the boundary (a.line bytes: a cache line, or 16) before the row of logits, so that a wavefront's
+// accesses go to whole lines wherever a row begins (those of the gradient too where it is laid out like the logits; by the gradient's own
+// boundary, the sums of a call without it would have other last bits).  What is left of the row before its first whole vector
+// and behind its last, fewer than N elements each, is its edge, an element each for lanes 0 to 7 and 8 to 15.
+template <class T>
+struct RowSpan {
+    static constexpr uint32_t N = 16 / sizeof(T);
+    int32_t shift;               // elements between the boundary and the row
+    uint32_t first, end;         // the whole vectors' numbers
+    uint32_t edge;               // this lane's edge element, or vocab
+    __device__ __forceinline__ RowSpan(const LossArgs &a, uintptr_t at, uint32_t lane)
+    {
+        shift = (int32_t)(((uint32_t)at & (a.line - 1u)) / (uint32_t)sizeof(T));
+        first = ((uint32_t)shift + N - 1u) / N;
+        end = ((uint32_t)shift + a.vocab) / N;
+        const uint32_t head = min(first * N - (uint32_t)shift, a.vocab);         // (first may lie behind end: a row inside one vector)
+        const uint32_t tail = end > first ? end * N - (uint32_t)shift : head;
+        edge = lane < 8u ? (lane < head ? lane : a.vocab) : lane < 16u ? min(tail + lane - 8u, a.vocab) : a.vocab;
+    }
+    // the lane that has an element
+    template <int SHARE>
+    __device__ __forceinline__ uint32_t owner(uint32_t i) const
+    {
+        const uint32_t head = first * N - (uint32_t)shift, v = (i + (uint32_t)shift) / N;
+        return i < head ? i : v < end ? v % SHARE : 8u + i - (end > first ? end * N - (uint32_t)shift : head);
+    }
+};
+
+// SHARE threads to a row, each with up to NV 16-byte vectors of it, which are read once, and perhaps an element of its edge.
+// KEEP: the exponentials stay in registers between the sum and the gradient, else the logits do.  HERE: the last block adds up
+// the rows' terms.
 template <class T, int SHARE, int NV, bool KEEP, bool LOSS, bool HERE>
 __global__ __launch_bounds__(SHARE < kBlock ? kBlock : SHARE, NV <= 4 ? 8 : 4) void loss_held_k(LossArgs a)
 {
     constexpr int THREADS = SHARE < kBlock ? kBlock : SHARE, N = Raw<T>::N, WAVES = SHARE / 64;
+    constexpr bool ONE = SHARE >= 64;
     typedef typename VecOf<T, N>::type out_vec;
     __shared__ float at[2 * WAVES + 1];
-    const uint32_t lane = threadIdx.x % SHARE, vecs = a.vocab / N, rest = a.vocab % N;
-    const uint32_t r = blockIdx.x * (THREADS / SHARE) + __builtin_amdgcn_readfirstlane(threadIdx.x / SHARE);
+    const uint32_t lane = threadIdx.x % SHARE, mine = threadIdx.x / SHARE;
+    const uint32_t r = blockIdx.x * (THREADS / SHARE) + (ONE ? (uint32_t)__builtin_amdgcn_readfirstlane(mine) : mine);
     auto body = [&] {
-        const Row row = row_of<LOSS>(a, r);
-        const global_ptr<const T> x = in_global(static_cast<const T *>(a.logits)) + (int64_t)r * a.stride;
-        const global_ptr<T> dx = in_global(static_cast<T *>(a.dlogits)) + (int64_t)r * a.dstride;
+        const Row row = row_of<LOSS, ONE>(a, r);
+        const T *rx = static_cast<const T *>(a.logits) + (int64_t)r * a.stride;
+        T *rd = static_cast<T *>(a.dlogits) + (int64_t)r * a.dstride;
+        const bool slopes = LOSS && a.dlogits != nullptr;
+        const RowSpan<T> span(a, (uintptr_t)rx, lane);
+        const global_ptr<const T> x = in_global(rx);
+        const global_ptr<T> dx = in_global(rd);
+        auto whole = [&](int k) { const uint32_t i = (uint32_t)k * SHARE + lane; return i >= span.first && i < span.end; };
+        auto place = [&](int k) { return (int64_t)((uint32_t)k * SHARE + lane) * N - span.shift; };
         auto put = [&](const Term &t) { if (HERE) leave_term(a.terms + r, t); else a.terms[r] = t; };
         if (!row.taken(a)) {
             if (lane == 0) {
                 if (LOSS) put({0.0f, 0.0f, row.weight, row.weight != 0.0f ? (uint32_t)TERM_LEFT_OUT : (uint32_t)TERM_NONE});
                 if (a.logp) a.logp[r] = 0.0f;
             }
-            if (LOSS && a.dlogits) {
+            if (slopes) {
                 const out_vec zero = {};
-                for (uint32_t i = lane; i < vecs; i += SHARE) __builtin_nontemporal_store(zero, (global_ptr<out_vec>)(dx + (size_t)i * N));
-                if (lane < rest) dx[vecs * N + lane] = (T)0.0f;
+#pragma unroll
+                for (int k = 0; k < NV; ++k) if (whole(k)) __builtin_nontemporal_store(zero, (global_ptr<out_vec>)(dx + place(k)));
+                if (span.edge < a.vocab) dx[span.edge] = (T)0.0f;
             }
             return;
         }
         Raw<T> raw[NV];
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const uint32_t i = (uint32_t)k * SHARE + lane;
-            if (i < vecs) raw[k].load(x + (size_t)i * N); else raw[k].none();
-        }
-        const float last = lane < rest ? (float)x[vecs * N + lane] : kNone;
+        for (int k = 0; k < NV; ++k) if (whole(k)) raw[k].load(x + place(k)); else raw[k].none();
+        const float edge = span.edge < a.vocab ? (float)x[span.edge] : kNone;
         float xa = (float)x[row.label];
         Largest<T> seen;
 #pragma unroll
         for (int k = 0; k < NV; ++k) seen.see(raw[k]);
-        const float wtop = wave_max(fmaxf(seen.get(), last)), wbase = base_of(wtop);
+        const float wtop = share_max<SHARE>(fmaxf(seen.get(), edge)), wbase = base_of(wtop);
         if (sizeof(T) < 4)
 #pragma unroll
             for (int k = 0; k < NV; ++k) raw[k].forget();
-        float e[KEEP ? NV * N : 1], sum = row_exp<T>(a, last, wbase);
-        const float elast = sum;
+        float e[KEEP ? NV * N : 1], sum = row_exp<T>(a, edge, wbase);
+        const float eedge = sum;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -283,9 +343,9 @@ __global__ __launch_bounds__(SHARE < kBlock ? kBlock : SHARE, NV <= 4 ? 8 : 4) v
                 if (KEEP) e[k * N + j] = y;
                 sum += y;
             }
-        sum = wave_sum_f(sum);
-        // The wavefronts' maxima and sums, and the label's logit as the first
-        // wavefront has read it: where the gradient takes the logits' place, another one may have overwritten it behind the barrier.
+        sum = share_sum<SHARE>(sum);
+        // The wavefronts' maxima and sums, and the label's logit as the first wavefront has read it: where the gradient takes the
+        // logits' place, another one may have overwritten it behind the barrier.
         float top = wbase, part = 1.0f;
         if constexpr (WAVES > 1) {
             if ((threadIdx.x & 63u) == 0) { at[lane >> 6] = wtop; at[WAVES + (lane >> 6)] = sum; }
@@ -293,21 +353,16 @@ __global__ __launch_bounds__(SHARE < kBlock ? kBlock : SHARE, NV <= 4 ? 8 : 4) v
             __syncthreads();
             xa = at[2 * WAVES];
             const float m = at[lane % WAVES];
-            top = m;
-#pragma unroll
-            for (int w = WAVES / 2; w >= 1; w >>= 1) top = fmaxf(top, __shfl_xor(top, w, 64));
-            top = base_of(top);
-            sum = at[WAVES + lane % WAVES] * row_exp<T>(a, m, top);
-#pragma unroll
-            for (int w = WAVES / 2; w >= 1; w >>= 1) sum += __shfl_xor(sum, w, 64);
+            top = base_of(share_max<WAVES>(m));
+            sum = share_sum<WAVES>(at[WAVES + lane % WAVES] * row_exp<T>(a, m, top));
             part = row_exp<T>(a, wtop, top);
         }
         const double l = ((double)xa - (double)top) * a.inv_t - log_wide(sum);
         if (lane == 0 && a.logp) a.logp[r] = (float)l;
         if (!LOSS) return;
-        const RowTerms t = row_terms(a, r, l);
+        const RowTerms t = row_terms(a, row, l);
         if (lane == 0) put({t.policy, t.kl, row.weight, t.cut ? (uint32_t)TERM_CUT : (uint32_t)TERM_FREE});
-        if (!a.dlogits) return;
+        if (!slopes) return;
         const float slope = row.weight * t.slope * a.gscale;
         part *= -slope / sum;
         if (!KEEP)
@@ -315,16 +370,14 @@ __global__ __launch_bounds__(SHARE < kBlock ? kBlock : SHARE, NV <= 4 ? 8 : 4) v
             for (int k = 0; k < NV; ++k) raw[k].forget();
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const uint32_t i = (uint32_t)k * SHARE + lane;
             out_vec v;
 #pragma unroll
             for (int j = 0; j < N; ++j) v[j] = (T)(part * (KEEP ? e[k * N + j] : row_exp<T>(a, raw[k].at(j), wbase)));
-            if (i < vecs) __builtin_nontemporal_store(v, (global_ptr<out_vec>)(dx + (size_t)i * N));
+            if (whole(k)) __builtin_nontemporal_store(v, (global_ptr<out_vec>)(dx + place(k)));
         }
-        if (lane < rest) dx[vecs * N + lane] = (T)(part * elast);
+        if (span.edge < a.vocab) dx[span.edge] = (T)(part * eedge);
         // the label's own element, by the thread that has stored it with the others
-        const uint32_t label = (uint32_t)row.label;
-        if (lane == (label < vecs * N ? label / N % SHARE : label - vecs * N)) dx[label] = (T)(part * row_exp<T>(a, xa, wbase) + slope);
+        if (lane == span.template owner<SHARE>((uint32_t)row.label)) dx[row.label] = (T)(part * row_exp<T>(a, xa, wbase) + slope);
     };
     if (r < a.rows) body();
     if (HERE) sum_here(a);
@@ -339,7 +392,7 @@ __global__ __launch_bounds__(kBlock) void loss_long_k(LossArgs a)
     __shared__ float lds[2 * kWavesPerBlock + 1];
     const uint32_t r = blockIdx.x;
     auto body = [&] {
-        const Row row = row_of<LOSS>(a, r);
+        const Row row = row_of<LOSS, true>(a, r);
         const global_ptr<const T> x = in_global(static_cast<const T *>(a.logits)) + (int64_t)r * a.stride;
         const global_ptr<T> dx = in_global(static_cast<T *>(a.dlogits)) + (int64_t)r * a.dstride;
         auto put = [&](const Term &t) { if (HERE) leave_term(a.terms + r, t); else a.terms[r] = t; };
@@ -383,7 +436,7 @@ __global__ __launch_bounds__(kBlock) void loss_long_k(LossArgs a)
         const double l = ((double)xa - (double)top) * a.inv_t - log_wide(sum);
         if (threadIdx.x == 0 && a.logp) a.logp[r] = (float)l;
         if (!LOSS) return;
-        const RowTerms t = row_terms(a, r, l);
+        const RowTerms t = row_terms(a, row, l);
         if (threadIdx.x == 0) put({t.policy, t.kl, row.weight, t.cut ? (uint32_t)TERM_CUT : (uint32_t)TERM_FREE});
         if (!a.dlogits) return;
         const float slope = row.weight * t.slope * a.gscale, part = -slope / sum;
@@ -412,11 +465,24 @@ static bool held(const LaunchCtx &lc, const LossArgs &a)
     launch(here ? loss_held_k<T, SHARE, NV, KEEP, LOSS, LOSS> : loss_held_k<T, SHARE, NV, KEEP, LOSS, false>, dim3(blocks), dim3(THREADS), lc.stream, a);
     return here;
 }
+// Vectors that the longest row may reach over, counted from a boundary of `line` bytes.
+template <class T>
+static uint32_t reach(const LossArgs &a, uint32_t line)
+{
+    const uintptr_t at = (uintptr_t)a.logits, step = (uintptr_t)a.stride * sizeof(T);
+    const uintptr_t shift = step % line == 0 ? at % line : line - sizeof(T);
+    return (uint32_t)((shift / sizeof(T) + a.vocab) / Raw<T>::N);
+}
 // At most kTermRows rows; whether their terms are added up.
 template <class T, bool LOSS>
-static bool loss_of(const LaunchCtx &lc, const LossArgs &a)
+static bool loss_of(const LaunchCtx &lc, LossArgs a)
 {
-    const uint32_t vecs = a.vocab / Raw<T>::N;
+    a.line = kLine;
+    // (a row that would need twice the registers for it is not moved to a line)
+    const uint32_t close = reach<T>(a, 16u);
+    uint32_t vecs = reach<T>(a, kLine);
+    for (uint32_t room : {16u, 64u, 128u, 256u, 512u, 1024u, 2048u, 4096u, 8192u, 16384u}) if (close <= room && room < vecs) { a.line = 16u; vecs = close; }
+    if (vecs <= 16 * 1) return held<T, 16, 1, true, LOSS>(lc, a);
     if (vecs <= 64 * 1) return held<T, 64, 1, true, LOSS>(lc, a);
     if (vecs <= 64 * 2) return held<T, 64, 2, true, LOSS>(lc, a);
     if (vecs <= 64 * 4) return held<T, 64, 4, true, LOSS>(lc, a);

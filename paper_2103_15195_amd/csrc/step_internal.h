@@ -65,6 +65,7 @@ struct LossArgs {
     Term *terms;                             // kTermRows
     double *partial;                         // kLossSums lists of kLossPartials sums, then the sums of the rows before these
     uint32_t *counts;                        // kArriveBytes
+    uint32_t line;                           // bytes: what rows' vectors are counted from a multiple of
     bool more;                               // there are rows before these
 };
 void launch_token_logp(const LaunchCtx &lc, int dtype, const LossArgs &a);
