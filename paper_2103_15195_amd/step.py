@@ -10,10 +10,12 @@ from __future__ import annotations
 import ctypes as C
 from typing import Optional, Sequence, Tuple
 
+import torch
+
 from . import binding as B
 
 MC_DTYPE_NONE, MC_DTYPE_F32, MC_DTYPE_BF16, MC_DTYPE_F16 = -1, 0, 1, 2
-DTYPE_IDS = {"float32": 0, "bfloat16": 1, "float16": 2}
+DTYPE_IDS = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 LISTS = {"grads": 0, "clipped": 1, "params": 2, "exp_avg": 3, "exp_avg_sq": 4, "model": 5}
 
 EXPORTS = ["mc_step_create", "mc_step_destroy", "mc_step_bind", "mc_grad_norm", "mc_grad_clip", "mc_adamw",
@@ -63,21 +65,28 @@ def dtype_id(dtype) -> int:
     """mc_dtype of a torch dtype or its name; None: no type."""
     if dtype is None:
         return MC_DTYPE_NONE
-    name = str(dtype).replace("torch.", "")
-    if name not in DTYPE_IDS:
-        raise ValueError(f"{dtype}: one of {', '.join(DTYPE_IDS)}")
-    return DTYPE_IDS[name]
+    kind = getattr(torch, dtype, dtype) if isinstance(dtype, str) else dtype
+    if kind not in DTYPE_IDS:
+        raise ValueError(f"{dtype}: one of {', '.join(map(str, DTYPE_IDS))}")
+    return DTYPE_IDS[kind]
 
 
-def _kind(tensor) -> str:
-    return str(tensor.dtype).replace("torch.", "")
+_F32, _I64 = torch.float32, torch.int64
 
 
-def _vector(tensor, name: str, count: int, kind: str = "float32"):
+def _vector(tensor, name: str, count: int, kind=_F32) -> int:
     """The address of a contiguous device tensor of `count` elements."""
-    if not tensor.is_cuda or _kind(tensor) != kind or tensor.numel() != count or not tensor.is_contiguous():
-        raise ValueError(f"{name}: {count} contiguous {kind} values on the device, not {tuple(tensor.shape)} of {tensor.dtype} on {tensor.device}")
+    if tensor.dtype is not kind or tensor.numel() != count or not tensor.is_cuda or not tensor.is_contiguous():
+        raise ValueError(f"{name}: {count} contiguous values of {kind} on the device, not {tuple(tensor.shape)} of {tensor.dtype} on {tensor.device}")
     return tensor.data_ptr()
+
+
+def _rows(x, name: str):
+    """(rows, columns, elements from row to row) of a two-dimensional tensor whose rows are contiguous."""
+    shape, step = x.shape, x.stride()
+    if len(shape) != 2 or not x.is_cuda or x.dtype not in DTYPE_IDS or (step[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{name}: rows of contiguous values on the device, of {', '.join(map(str, DTYPE_IDS))}, not {tuple(shape)} of {x.dtype} on {x.device}")
+    return shape[0], shape[1], step[0] if shape[0] > 1 else max(step[0], shape[1])
 
 
 class Step:
@@ -127,7 +136,7 @@ class Step:
             if len(tensors) != len(self.numel):
                 raise ValueError(f"{name}: {len(self.numel)} tensors, not {len(tensors)}")
             for i, (t, n) in enumerate(zip(tensors, self.numel)):
-                if t.numel() != n or not t.is_contiguous() or not t.is_cuda or DTYPE_IDS.get(_kind(t)) != self.dtypes[name]:
+                if t.numel() != n or not t.is_contiguous() or not t.is_cuda or DTYPE_IDS.get(t.dtype) != self.dtypes[name]:
                     raise ValueError(f"{name}[{i}]: {n} contiguous elements on the device of the list's type, not {tuple(t.shape)} of {t.dtype} on {t.device}")
         for name, tensors in lists.items():
             tensors = list(tensors)
@@ -167,39 +176,30 @@ class PolicyLoss:
         except Exception:
             pass
 
-    @staticmethod
-    def _rows(x, name: str):
-        """(rows, columns, elements from row to row) of a two-dimensional tensor whose rows are contiguous."""
-        if x.dim() != 2 or not x.is_cuda or _kind(x) not in DTYPE_IDS or (x.shape[1] > 1 and x.stride(1) != 1):
-            raise ValueError(f"{name}: rows of contiguous values on the device, of {', '.join(DTYPE_IDS)}, not {tuple(x.shape)} of {x.dtype} on {x.device}")
-        rows, columns = x.shape
-        return rows, columns, x.stride(0) if rows > 1 else max(x.stride(0), columns)
-
-    def _logits(self, logits, labels, temperature):
-        rows, vocab, stride = self._rows(logits, "logits")
-        return McLogits(logits.data_ptr(), _vector(labels, "labels", rows, "int64"), rows, vocab, stride, DTYPE_IDS[_kind(logits)], temperature)
-
     def mc_token_logp(self, logits, labels, logp, temperature: float = 1.0, stream=None) -> None:
         """logp[r] = log-probability of labels[r] under logits[r] / temperature; 0 where the label is none of the row's."""
-        x = self._logits(logits, labels, temperature)
-        B._check(lib().mc_token_logp(self._h, C.byref(x), _vector(logp, "logp", x.rows), B._stream_handle(stream)), "mc_token_logp")
+        rows, vocab, stride = _rows(logits, "logits")
+        x = McLogits(logits.data_ptr(), _vector(labels, "labels", rows, _I64), rows, vocab, stride, DTYPE_IDS[logits.dtype], temperature)
+        rc = lib().mc_token_logp(self._h, C.byref(x), _vector(logp, "logp", rows), B._stream_handle(stream))
+        if rc:
+            raise B.McError(rc, "mc_token_logp")
 
     def mc_policy_loss(self, logits, labels, old_logp, advantages, *, sums, weights=None, ref_logp=None, clip: Tuple[float, float] = (0.2, 0.2),
                        kl_coef: float = 0.0, temperature: float = 1.0, grad_scale: float = 1.0, logp=None, dlogits=None, stream=None) -> None:
         """The loss of mergecomp_step.h and, in dlogits (which may be the logits), grad_scale times its gradient.
         sums: 8 floats on the device: loss, policy term, KL term, clipped weight, weight; as int32 rows that took part, rows
         whose label is none of the row's; 0."""
-        x = self._logits(logits, labels, temperature)
-        n, p = x.rows, McPolicy()
-        p.old_logp, p.advantages = _vector(old_logp, "old_logp", n), _vector(advantages, "advantages", n)
-        p.weights = None if weights is None else _vector(weights, "weights", n)
-        p.ref_logp = None if ref_logp is None else _vector(ref_logp, "ref_logp", n)
-        p.clip_low, p.clip_high, p.kl_coef, p.grad_scale = clip[0], clip[1], kl_coef, grad_scale
-        p.sums = _vector(sums, "sums", 8)
-        p.logp = None if logp is None else _vector(logp, "logp", n)
+        rows, vocab, stride = _rows(logits, "logits")
+        x = McLogits(logits.data_ptr(), _vector(labels, "labels", rows, _I64), rows, vocab, stride, DTYPE_IDS[logits.dtype], temperature)
+        slopes, dstride = None, 0
         if dlogits is not None:
-            rows, vocab, p.dlogits_stride = self._rows(dlogits, "dlogits")
-            if (rows, vocab) != (x.rows, x.vocab) or dlogits.dtype != logits.dtype:
+            drows, dvocab, dstride = _rows(dlogits, "dlogits")
+            if drows != rows or dvocab != vocab or dlogits.dtype is not logits.dtype:
                 raise ValueError(f"dlogits: the logits' shape and type, not {tuple(dlogits.shape)} of {dlogits.dtype}")
-            p.dlogits = dlogits.data_ptr()
-        B._check(lib().mc_policy_loss(self._h, C.byref(x), C.byref(p), B._stream_handle(stream)), "mc_policy_loss")
+            slopes = dlogits.data_ptr()
+        p = McPolicy(_vector(old_logp, "old_logp", rows), _vector(advantages, "advantages", rows),
+                     None if weights is None else _vector(weights, "weights", rows), None if ref_logp is None else _vector(ref_logp, "ref_logp", rows),
+                     clip[0], clip[1], kl_coef, grad_scale, _vector(sums, "sums", 8), None if logp is None else _vector(logp, "logp", rows), slopes, dstride)
+        rc = lib().mc_policy_loss(self._h, C.byref(x), C.byref(p), B._stream_handle(stream))
+        if rc:
+            raise B.McError(rc, "mc_policy_loss")
