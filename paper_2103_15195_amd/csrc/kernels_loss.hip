@@ -183,11 +183,9 @@ template <> struct Raw<float> {
     typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
     float x[4];
     __device__ __forceinline__ void none() { for (int e = 0; e < N; ++e) x[e] = kNone; }
-    __device__ __forceinline__ void load(global_ptr<const float> p)
-    {
-        const vec v = __builtin_nontemporal_load((global_ptr<const vec>)p);
-        for (int e = 0; e < N; ++e) x[e] = v[e];
-    }
+    __device__ __forceinline__ void take(vec v) { for (int e = 0; e < N; ++e) x[e] = v[e]; }
+    __device__ __forceinline__ void load(global_ptr<const float> p) { take(__builtin_nontemporal_load((global_ptr<const vec>)p)); }
+    __device__ __forceinline__ void load_cached(global_ptr<const float> p) { take(*(global_ptr<const vec>)p); }
     __device__ __forceinline__ float at(int e) const { return x[e]; }
     __device__ __forceinline__ void forget() { for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(x[e])); }
 };
@@ -211,11 +209,9 @@ template <class T> struct Raw {
     __device__ __forceinline__ void forget() { for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(x[e])); }
     static constexpr uint32_t kNoneBits = std::is_same_v<T, __bf16> ? 0xFF80FF80u : 0xFC00FC00u;
     __device__ __forceinline__ void none() { for (int e = 0; e < 4; ++e) x[e] = kNoneBits; }
-    __device__ __forceinline__ void load(global_ptr<const T> p)
-    {
-        const vec v = __builtin_nontemporal_load((global_ptr<const vec>)p);
-        for (int e = 0; e < 4; ++e) x[e] = v[e];
-    }
+    __device__ __forceinline__ void take(vec v) { for (int e = 0; e < 4; ++e) x[e] = v[e]; }
+    __device__ __forceinline__ void load(global_ptr<const T> p) { take(__builtin_nontemporal_load((global_ptr<const vec>)p)); }
+    __device__ __forceinline__ void load_cached(global_ptr<const T> p) { take(*(global_ptr<const vec>)p); }
     __device__ __forceinline__ float at(int e) const
     {
         if constexpr (std::is_same_v<T, __bf16>) return __uint_as_float(e & 1 ? x[e >> 1] & 0xFFFF0000u : x[e >> 1] << 16);
@@ -384,75 +380,217 @@ __global__ __launch_bounds__(SHARE < kBlock ? kBlock : SHARE, NV <= 4 ? 8 : 4) v
 }
 
 // ---- longer rows --------------------------------------------------------------------------------------------------------------
-// One block to a row, two passes over it: the running maximum and sum, then the gradient.
+// As above, by 1024 threads, of which each holds NV vectors; what lies behind those is read twice, by way of the caches: with a block to a compute
+// unit, 256 rows of 400 KB are under way, and what is read again of them stays in the last-level cache.  1024 rows of 200001 bf16 138 us, 256 of 262144
+// fp32 97 (with 8 vectors held 147 and 97, two read ahead instead of four 144 and 97; 256 threads that held nothing 245 and 333).
 template <class T, bool LOSS, bool HERE>
-__global__ __launch_bounds__(kBlock) void loss_long_k(LossArgs a)
+__global__ __launch_bounds__(1024, LOSS ? 4 : 8) void loss_long_k(LossArgs a)
 {
-    constexpr int N = 16 / (int)sizeof(T);
-    __shared__ float lds[2 * kWavesPerBlock + 1];
-    const uint32_t r = blockIdx.x;
+    constexpr int SHARE = 1024, NV = LOSS ? 16 : 4, AHEAD = 4, N = Raw<T>::N, WAVES = SHARE / 64;
+    typedef typename VecOf<T, N>::type out_vec;
+    __shared__ float at[2 * WAVES + 1];
+    const uint32_t lane = threadIdx.x, r = blockIdx.x;
     auto body = [&] {
         const Row row = row_of<LOSS, true>(a, r);
-        const global_ptr<const T> x = in_global(static_cast<const T *>(a.logits)) + (int64_t)r * a.stride;
-        const global_ptr<T> dx = in_global(static_cast<T *>(a.dlogits)) + (int64_t)r * a.dstride;
+        const T *rx = static_cast<const T *>(a.logits) + (int64_t)r * a.stride;
+        T *rd = static_cast<T *>(a.dlogits) + (int64_t)r * a.dstride;
+        const bool slopes = LOSS && a.dlogits != nullptr;
+        const RowSpan<T> span(a, (uintptr_t)rx, lane);
+        const global_ptr<const T> x = in_global(rx);
+        const global_ptr<T> dx = in_global(rd);
+        auto place = [&](uint32_t i) { return (int64_t)i * N - span.shift; };
         auto put = [&](const Term &t) { if (HERE) leave_term(a.terms + r, t); else a.terms[r] = t; };
         if (!row.taken(a)) {
-            if (threadIdx.x == 0) {
+            if (lane == 0) {
                 if (LOSS) put({0.0f, 0.0f, row.weight, row.weight != 0.0f ? (uint32_t)TERM_LEFT_OUT : (uint32_t)TERM_NONE});
                 if (a.logp) a.logp[r] = 0.0f;
             }
-            if (LOSS && a.dlogits) {
-                const float zero[N] = {};
-                for (uint32_t i = threadIdx.x * N; i < a.vocab; i += kBlock * N) store_some<N, T>(dx, (int32_t)i, 0, (int32_t)a.vocab, zero);
+            if (slopes) {
+                const out_vec zero = {};
+                for (uint32_t i = lane; i < span.end; i += SHARE) if (i >= span.first) __builtin_nontemporal_store(zero, (global_ptr<out_vec>)(dx + place(i)));
+                if (span.edge < a.vocab) dx[span.edge] = (T)0.0f;
             }
             return;
         }
-        float xa = (float)x[row.label], top = kNone, sum = 0.0f;
-        for (uint32_t i = threadIdx.x * N; i < a.vocab; i += kBlock * N) {
-            float v[N], most;
-            load_some<N, T>(x, (int32_t)i, 0, (int32_t)a.vocab, v, kNone);
-            most = v[0];
+        Raw<T> raw[NV];
 #pragma unroll
-            for (int e = 1; e < N; ++e) most = fmaxf(most, v[e]);
-            if (most > top) { sum *= row_exp<T>(a, top, most); top = most; }
+        for (int k = 0; k < NV; ++k) {
+            const uint32_t i = (uint32_t)k * SHARE + lane;
+            if (i >= span.first && i < span.end) raw[k].load(x + place(i)); else raw[k].none();
+        }
+        const float edge = span.edge < a.vocab ? (float)x[span.edge] : kNone;
+        float xa = (float)x[row.label];
+        // the running maximum and sum of what is not held
+        float top = kNone, sum = 0.0f;
+        for (uint32_t i = (uint32_t)NV * SHARE + lane; i < span.end; i += SHARE * AHEAD) {
+            Raw<T> next[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) if (i + SHARE * k < span.end) next[k].load_cached(x + place(i + SHARE * k)); else next[k].none();
+            Largest<T> seen;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) seen.see(next[k]);
+            const float most = seen.get();
+            if (!(most <= top)) { sum *= row_exp<T>(a, top, base_of(most)); top = most; }
             const float base = base_of(top);
 #pragma unroll
-            for (int e = 0; e < N; ++e) sum += row_exp<T>(a, v[e], base);
+            for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                for (int j = 0; j < N; ++j) sum += row_exp<T>(a, next[k].at(j), base);
         }
-        const float wtop = wave_max(top);
-        sum = wave_sum_f(sum * row_exp<T>(a, top, base_of(wtop)));
-        if ((threadIdx.x & 63u) == 0) { lds[threadIdx.x >> 6] = wtop; lds[kWavesPerBlock + (threadIdx.x >> 6)] = sum; }
-        if (threadIdx.x == 0) lds[2 * kWavesPerBlock] = xa;      // (see above)
-        __syncthreads();
-        xa = lds[2 * kWavesPerBlock];
-        top = lds[0];
+        Largest<T> seen;
 #pragma unroll
-        for (int k = 1; k < kWavesPerBlock; ++k) top = fmaxf(top, lds[k]);
-        top = base_of(top);
-        sum = 0.0f;
+        for (int k = 0; k < NV; ++k) seen.see(raw[k]);
+        const float wtop = share_max<64>(fmaxf(fmaxf(seen.get(), edge), top)), wbase = base_of(wtop);
+        const float eedge = row_exp<T>(a, edge, wbase);
+        sum = sum * row_exp<T>(a, top, wbase) + eedge;
 #pragma unroll
-        for (int k = 0; k < kWavesPerBlock; ++k) sum += lds[kWavesPerBlock + k] * row_exp<T>(a, lds[k], top);
+        for (int k = 0; k < NV; ++k) {
+            raw[k].forget();
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum += row_exp<T>(a, raw[k].at(j), wbase);
+        }
+        sum = share_sum<64>(sum);
+        if ((threadIdx.x & 63u) == 0) { at[lane >> 6] = wtop; at[WAVES + (lane >> 6)] = sum; }
+        if (lane == 0) at[2 * WAVES] = xa;              // (see above)
         __syncthreads();
+        xa = at[2 * WAVES];
+        const float m = at[lane % WAVES];
+        top = base_of(share_max<WAVES>(m));
+        sum = share_sum<WAVES>(at[WAVES + lane % WAVES] * row_exp<T>(a, m, top));
         const double l = ((double)xa - (double)top) * a.inv_t - log_wide(sum);
-        if (threadIdx.x == 0 && a.logp) a.logp[r] = (float)l;
+        if (lane == 0 && a.logp) a.logp[r] = (float)l;
         if (!LOSS) return;
         const RowTerms t = row_terms(a, row, l);
-        if (threadIdx.x == 0) put({t.policy, t.kl, row.weight, t.cut ? (uint32_t)TERM_CUT : (uint32_t)TERM_FREE});
-        if (!a.dlogits) return;
+        if (lane == 0) put({t.policy, t.kl, row.weight, t.cut ? (uint32_t)TERM_CUT : (uint32_t)TERM_FREE});
+        if (!slopes) return;
         const float slope = row.weight * t.slope * a.gscale, part = -slope / sum;
-        for (uint32_t i = threadIdx.x * N; i < a.vocab; i += kBlock * N) {
-            float v[N];
-            load_some<N, T>(x, (int32_t)i, 0, (int32_t)a.vocab, v, kNone);
+        auto store = [&](uint32_t i, const Raw<T> &v) {
+            out_vec o;
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                v[e] = part * row_exp<T>(a, v[e], top);
-                if (i + (uint32_t)e == (uint32_t)row.label) v[e] += slope;
-            }
-            store_some<N, T>(dx, (int32_t)i, 0, (int32_t)a.vocab, v);
+            for (int j = 0; j < N; ++j) o[j] = (T)(part * row_exp<T>(a, v.at(j), top));
+            __builtin_nontemporal_store(o, (global_ptr<out_vec>)(dx + place(i)));
+        };
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            raw[k].forget();
+            const uint32_t i = (uint32_t)k * SHARE + lane;
+            if (i >= span.first && i < span.end) store(i, raw[k]);
         }
+        for (uint32_t i = (uint32_t)NV * SHARE + lane; i < span.end; i += SHARE * AHEAD) {
+            Raw<T> next[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) if (i + SHARE * k < span.end) next[k].load(x + place(i + SHARE * k));
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) if (i + SHARE * k < span.end) store(i + SHARE * k, next[k]);
+        }
+        if (span.edge < a.vocab) dx[span.edge] = (T)(part * row_exp<T>(a, edge, top));
+        if (lane == span.template owner<SHARE>((uint32_t)row.label)) dx[row.label] = (T)(part * row_exp<T>(a, xa, top) + slope);
     };
     body();
     if (HERE) sum_here(a);
+}
+
+// ---- few rows -----------------------------------------------------------------------------------------------------------------
+// A row by as many blocks as it has parts of kPartVecs vectors: each finds its part's maximum and sum, and a second launch, where they
+// are joined, reads the part again, which the caches still hold, and writes the gradient.
+constexpr int kPartSteps = 4;
+constexpr uint32_t kPartVecs = kPartSteps * kBlock;
+template <class T>
+__global__ __launch_bounds__(kBlock) void loss_parts_k(LossArgs a, uint32_t parts)
+{
+    __shared__ float at[2 * kWavesPerBlock];
+    const uint32_t r = blockIdx.x / parts, part = blockIdx.x % parts, lane = threadIdx.x;
+    const Row row = row_of<false, true>(a, r);
+    if (!row.valid(a) || (a.weights && ld_uniform(a.weights + r) == 0.0f)) return;
+    const T *rx = static_cast<const T *>(a.logits) + (int64_t)r * a.stride;
+    const global_ptr<const T> x = in_global(rx);
+    const RowSpan<T> span(a, (uintptr_t)rx, lane);
+    Raw<T> raw[kPartSteps];
+#pragma unroll
+    for (int k = 0; k < kPartSteps; ++k) {
+        const uint32_t i = part * kPartVecs + (uint32_t)k * kBlock + lane;
+        if (i >= span.first && i < span.end) raw[k].load_cached(x + ((int64_t)i * Raw<T>::N - span.shift)); else raw[k].none();
+    }
+    const float edge = part == 0 && span.edge < a.vocab ? (float)x[span.edge] : kNone;
+    if (part == 0 && lane == 0) a.parts[r].label = (float)x[row.label];
+    Largest<T> seen;
+#pragma unroll
+    for (int k = 0; k < kPartSteps; ++k) seen.see(raw[k]);
+    const float wtop = share_max<64>(fmaxf(seen.get(), edge)), wbase = base_of(wtop);
+    float sum = row_exp<T>(a, edge, wbase);
+#pragma unroll
+    for (int k = 0; k < kPartSteps; ++k)
+#pragma unroll
+        for (int j = 0; j < Raw<T>::N; ++j) sum += row_exp<T>(a, raw[k].at(j), wbase);
+    sum = share_sum<64>(sum);
+    if ((lane & 63u) == 0) { at[lane >> 6] = wtop; at[kWavesPerBlock + (lane >> 6)] = sum; }
+    __syncthreads();
+    const float m = at[lane % kWavesPerBlock], top = share_max<kWavesPerBlock>(m);
+    sum = share_sum<kWavesPerBlock>(at[kWavesPerBlock + lane % kWavesPerBlock] * row_exp<T>(a, m, base_of(top)));
+    if (lane == 0) { a.parts[r].top[part] = top; a.parts[r].sum[part] = sum; }
+}
+// LOSS: a block to a part again; else one to a row.
+template <class T, bool LOSS>
+__global__ __launch_bounds__(kBlock) void loss_join_k(LossArgs a, uint32_t parts)
+{
+    constexpr int N = Raw<T>::N;
+    typedef typename VecOf<T, N>::type out_vec;
+    const uint32_t r = LOSS ? blockIdx.x / parts : blockIdx.x, part = LOSS ? blockIdx.x % parts : 0u, lane = threadIdx.x;
+    auto body = [&] {
+        const Row row = row_of<LOSS, true>(a, r);
+        const T *rx = static_cast<const T *>(a.logits) + (int64_t)r * a.stride;
+        T *rd = static_cast<T *>(a.dlogits) + (int64_t)r * a.dstride;
+        const bool slopes = LOSS && a.dlogits != nullptr;
+        const RowSpan<T> span(a, (uintptr_t)rx, lane);
+        const global_ptr<const T> x = in_global(rx);
+        const global_ptr<T> dx = in_global(rd);
+        auto number = [&](int k) { return part * kPartVecs + (uint32_t)k * kBlock + lane; };
+        auto whole = [&](int k) { const uint32_t i = number(k); return i >= span.first && i < span.end; };
+        auto place = [&](int k) { return (int64_t)number(k) * N - span.shift; };
+        const bool edges = part == 0 && span.edge < a.vocab, first = part == 0 && lane == 0;
+        if (!row.taken(a)) {
+            if (first && LOSS) leave_term(a.terms + r, {0.0f, 0.0f, row.weight, row.weight != 0.0f ? (uint32_t)TERM_LEFT_OUT : (uint32_t)TERM_NONE});
+            if (first && a.logp) a.logp[r] = 0.0f;
+            if (slopes) {
+                const out_vec zero = {};
+#pragma unroll
+                for (int k = 0; k < kPartSteps; ++k) if (whole(k)) __builtin_nontemporal_store(zero, (global_ptr<out_vec>)(dx + place(k)));
+                if (edges) dx[span.edge] = (T)0.0f;
+            }
+            return;
+        }
+        Raw<T> raw[kPartSteps];
+        float edge = kNone;
+        if (slopes) {
+#pragma unroll
+            for (int k = 0; k < kPartSteps; ++k) if (whole(k)) raw[k].load(x + place(k)); else raw[k].none();
+            if (edges) edge = (float)x[span.edge];
+        }
+        const PartsOfRow &of = a.parts[r];
+        const float xa = of.label, m = (lane & 63u) < parts ? of.top[lane & 63u] : kNone, s = (lane & 63u) < parts ? of.sum[lane & 63u] : 0.0f;
+        const float top = base_of(share_max<64>(m)), sum = share_sum<64>(s * row_exp<T>(a, m, top));
+        const double l = ((double)xa - (double)top) * a.inv_t - log_wide(sum);
+        if (first && a.logp) a.logp[r] = (float)l;
+        if (!LOSS) return;
+        const RowTerms t = row_terms(a, row, l);
+        if (first) leave_term(a.terms + r, {t.policy, t.kl, row.weight, t.cut ? (uint32_t)TERM_CUT : (uint32_t)TERM_FREE});
+        if (!slopes) return;
+        const float slope = row.weight * t.slope * a.gscale, scale = -slope / sum;
+#pragma unroll
+        for (int k = 0; k < kPartSteps; ++k) {
+            out_vec v;
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = (T)(scale * row_exp<T>(a, raw[k].at(j), top));
+            if (whole(k)) __builtin_nontemporal_store(v, (global_ptr<out_vec>)(dx + place(k)));
+        }
+        if (edges) dx[span.edge] = (T)(scale * row_exp<T>(a, edge, top));
+        // the label's own element, by the thread that has stored it with the others
+        const uint32_t i = ((uint32_t)row.label + (uint32_t)span.shift) / N;
+        const bool in_vector = i >= span.first && i < span.end;
+        if (part == (in_vector ? i / kPartVecs : 0u) && lane == span.template owner<kBlock>((uint32_t)row.label)) dx[row.label] = (T)(scale * row_exp<T>(a, xa, top) + slope);
+    };
+    body();
+    if (LOSS) sum_here(a);
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------------
@@ -474,6 +612,9 @@ static uint32_t reach(const LossArgs &a, uint32_t line)
     return (uint32_t)((shift / sizeof(T) + a.vocab) / Raw<T>::N);
 }
 // At most kTermRows rows; whether their terms are added up.
+// Threads to a row: as few as hold it in the registers that let 32 wavefronts share a compute unit (64), up to 65536 elements of 16 bits; of longer
+// rows twice that.  Rates of the policy loss in bf16 (TB/s): 4096 x 32064 5.4, 32003 (rows begin anywhere) 5.4, both with one row in eight masked; with 40 %
+// masked 4096 x 32064 5.2, 8192 x 8192 4.7, 16384 x 4096 4.9, 32768 x 1000 3.6, 65536 x 100 1.2, 2048 x 65536 5.0, 2048 x 128259 5.2, 1024 x 200001 4.9.
 template <class T, bool LOSS>
 static bool loss_of(const LaunchCtx &lc, LossArgs a)
 {
@@ -482,6 +623,17 @@ static bool loss_of(const LaunchCtx &lc, LossArgs a)
     const uint32_t close = reach<T>(a, 16u);
     uint32_t vecs = reach<T>(a, kLine);
     for (uint32_t room : {16u, 64u, 128u, 256u, 512u, 1024u, 2048u, 4096u, 8192u, 16384u}) if (close <= room && room < vecs) { a.line = 16u; vecs = close; }
+    // Few long rows are shared by blocks.  (Policy loss so and with a block to each, us: rows of 128256 bf16, 1 / 64 / 128 / 200 of them 13.6 / 14.0 / 19.0 / 27.5
+    // and 18.2 / 21.0 / 21.7 / 23.7; of 262144 fp32 13.6 / 30.8 / 56.9 / 88.3 and 42.9 / 51.6 / 71.0 / 97.0; of 70000 bf16, 64 / 128 / 200 13.1 / 15.1 / 17.6 and
+    // 17.1 / 17.6 / 18.3.  Below 8192 vectors the second launch costs more than it gains: 1 / 64 of 64000 bf16 13.5 / 13.3 and 11.8 / 14.0, their
+    // log-probabilities alone 8.6 / 8.7 and 6.3 / 7.4.)
+    const uint32_t parts = (reach<T>(a, kLine) + kPartVecs - 1u) / kPartVecs;
+    if (a.rows <= kPartRows && parts <= kMostParts && vecs > 1024 * 8 && !a.more) {
+        a.line = kLine;
+        launch(loss_parts_k<T>, dim3(a.rows * parts), dim3(kBlock), lc.stream, a, parts);
+        launch(loss_join_k<T, LOSS>, dim3(LOSS ? a.rows * parts : a.rows), dim3(LOSS ? kBlock : 64), lc.stream, a, parts);
+        return LOSS;
+    }
     if (vecs <= 16 * 1) return held<T, 16, 1, true, LOSS>(lc, a);
     if (vecs <= 64 * 1) return held<T, 64, 1, true, LOSS>(lc, a);
     if (vecs <= 64 * 2) return held<T, 64, 2, true, LOSS>(lc, a);
@@ -490,10 +642,11 @@ static bool loss_of(const LaunchCtx &lc, LossArgs a)
     if (vecs <= 256 * 4) return held<T, 256, 4, true, LOSS>(lc, a);
     if (vecs <= 1024 * 2) return held<T, 1024, 2, true, LOSS>(lc, a);
     if (vecs <= 1024 * 4) return held<T, 1024, 4, true, LOSS>(lc, a);
-    if (vecs <= 1024 * 8) return held<T, 1024, 8, false, LOSS>(lc, a);
-    if (vecs <= 1024 * 16) return held<T, 1024, 16, false, LOSS>(lc, a);
+    // (log-probabilities alone are read once in any case: 2048 rows of 128259 62 us held, 56 not)
+    if (LOSS && vecs <= 1024 * 8) return held<T, 1024, 8, false, LOSS>(lc, a);
+    if (LOSS && vecs <= 1024 * 16) return held<T, 1024, 16, false, LOSS>(lc, a);
     const bool here = LOSS && a.rows <= kFewBlocks && !a.more;
-    launch(here ? loss_long_k<T, LOSS, LOSS> : loss_long_k<T, LOSS, false>, dim3(a.rows), dim3(kBlock), lc.stream, a);
+    launch(here ? loss_long_k<T, LOSS, LOSS> : loss_long_k<T, LOSS, false>, dim3(a.rows), dim3(1024), lc.stream, a);
     return here;
 }
 // the sums of no rows

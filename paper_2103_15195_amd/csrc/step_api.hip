@@ -23,6 +23,7 @@ struct mc_step {
 struct mc_loss {
     int device = 0;
     Term *d_terms = nullptr;
+    PartsOfRow *d_parts = nullptr;
     double *d_partial = nullptr;
     uint32_t *d_counts = nullptr;        // 0 between calls
 };
@@ -196,6 +197,7 @@ int mc_loss_destroy(mc_loss *h)
         OnDevice guard(h->device);
         (void)hipDeviceSynchronize();
         if (h->d_terms) (void)hipFree(h->d_terms);
+        if (h->d_parts) (void)hipFree(h->d_parts);
         if (h->d_partial) (void)hipFree(h->d_partial);
         if (h->d_counts) (void)hipFree(h->d_counts);
     }
@@ -212,6 +214,7 @@ int mc_loss_create(mc_loss **out)
     if (hipGetDevice(&h->device) != hipSuccess) { (void)hipGetLastError(); delete h; return MC_ERR_DEVICE; }
     int rc = grab(&h->d_partial, (size_t)(kLossPartials + 1) * kLossSums * sizeof(double));
     if (rc == MC_OK) rc = grab(&h->d_terms, (size_t)kTermRows * sizeof(Term));
+    if (rc == MC_OK) rc = grab(&h->d_parts, (size_t)kPartRows * sizeof(PartsOfRow));
     if (rc == MC_OK) rc = grab_counts(&h->d_counts);
     if (rc != MC_OK) { mc_loss_destroy(h); return rc; }
     *out = h;
@@ -237,6 +240,7 @@ static int logits_args(const mc_loss *h, const mc_logits *x, LossArgs &a)
     a.inv_t = 1.0 / (double)x->temperature;
     a.partial = h->d_partial;
     a.terms = h->d_terms;
+    a.parts = h->d_parts;
     a.counts = h->d_counts;
     return MC_OK;
 }

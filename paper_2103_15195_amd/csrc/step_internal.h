@@ -51,6 +51,13 @@ enum TermKind { TERM_NONE = 0, TERM_FREE = 1, TERM_CUT = 2, TERM_LEFT_OUT = 3 };
 constexpr uint32_t kTermRows = 1u << 17;     // rows that there is room for: more of them are taken so many at a time
 constexpr uint32_t kTermBlock = 4096;        // rows per block of the kernel that adds them up
 constexpr uint32_t kLossPartials = kTermRows / kTermBlock;
+// The parts of a row that several blocks share.
+constexpr uint32_t kPartRows = 128, kMostParts = 64;
+struct PartsOfRow {
+    float top[kMostParts], sum[kMostParts];
+    float label;                             // the label's logit
+    float pad[31];
+};
 struct LossArgs {
     const void *logits;
     const int64_t *labels;
@@ -63,6 +70,7 @@ struct LossArgs {
     double inv_t;
     float lo, hi, kl_coef, gscale;           // gscale: grad_scale / temperature
     Term *terms;                             // kTermRows
+    PartsOfRow *parts;                       // kPartRows
     double *partial;                         // kLossSums lists of kLossPartials sums, then the sums of the rows before these
     uint32_t *counts;                        // kArriveBytes
     uint32_t line;                           // bytes: what rows' vectors are counted from a multiple of
