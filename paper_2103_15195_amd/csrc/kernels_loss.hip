@@ -84,33 +84,44 @@ __device__ __forceinline__ RowTerms row_terms(const LossArgs &a, const Row &row,
 // The rows' kernels leave a Term for every row.  In launches of few blocks the last one adds them up; in larger ones, where that
 // block would find thousands of them and every block would wait for its terms to be written through, a kernel behind them does.
 struct Sums {
-    double at[kLossSums] = {};
-    __device__ __forceinline__ void add(const Term &t, float kl_coef)
+    double at[4] = {};           // weight times policy term, KL term, whether the clamp decides, 1
+    uint32_t taken = 0, left_out = 0;
+    __device__ __forceinline__ void add(const Term &t)
     {
-        const bool taken = t.kind == TERM_FREE || t.kind == TERM_CUT;
-        const double w = taken ? (double)t.weight : 0.0;
-        if (taken) {
-            at[0] += w * ((double)t.policy + (double)kl_coef * t.kl);
-            at[1] += w * t.policy;
-            at[2] += w * t.kl;
-        }
-        at[3] += t.kind == TERM_CUT ? w : 0.0;
-        at[4] += w;
-        at[5] += taken ? 1.0 : 0.0;
-        at[6] += t.kind == TERM_LEFT_OUT ? 1.0 : 0.0;
+        const bool is_taken = t.kind == TERM_FREE || t.kind == TERM_CUT;
+        const double w = is_taken ? (double)t.weight : 0.0;
+        at[0] = __builtin_fma(w, is_taken ? (double)t.policy : 0.0, at[0]);
+        at[1] = __builtin_fma(w, is_taken ? (double)t.kl : 0.0, at[1]);
+        at[2] += t.kind == TERM_CUT ? w : 0.0;
+        at[3] += w;
+        taken += is_taken;
+        left_out += t.kind == TERM_LEFT_OUT;
     }
-    __device__ __forceinline__ void join()
+    // Over a wavefront, the sum with the number sum_of_lane() in every lane.  Lanes hand each other half of what they have, and go on with the other half.
+    __device__ __forceinline__ double join()
     {
+        const bool odd = threadIdx.x & 1u, odd2 = threadIdx.x & 2u;
+        double a = (odd ? at[2] : at[0]) + __shfl_xor(odd ? at[0] : at[2], 1, 64), b = (odd ? at[3] : at[1]) + __shfl_xor(odd ? at[1] : at[3], 1, 64);
+        a = (odd2 ? b : a) + __shfl_xor(odd2 ? a : b, 2, 64);
 #pragma unroll
-        for (int k = 0; k < kLossSums; ++k) at[k] = wave_sum(at[k]);
-    }
-    __device__ __forceinline__ void put(float *out) const
-    {
-#pragma unroll
-        for (int k = 0; k < kLossSums; ++k) out[k] = k < 5 ? (float)at[k] : __int_as_float((int)at[k]);
-        out[kLossSums] = 0.0f;
+        for (int m = 4; m <= 32; m <<= 1) a += __shfl_xor(a, m, 64);
+        taken = wave_sum_u32(taken);
+        left_out = wave_sum_u32(left_out);
+        return a;
     }
 };
+__device__ __forceinline__ uint32_t sum_of_lane() { return (threadIdx.x & 1u) * 2u + (threadIdx.x >> 1 & 1u); }
+// by a wavefront whose lane k < 4 has sum k, and lane 0 the counts
+__device__ __forceinline__ void put_sums(const LossArgs &a, double sum, uint32_t taken, uint32_t left_out)
+{
+    const double policy = __shfl(sum, 0, 64), kl = __shfl(sum, 1, 64);
+    if (threadIdx.x < 4u) a.sums[1u + threadIdx.x] = (float)sum;
+    if (threadIdx.x != 0) return;
+    a.sums[0] = (float)(a.ref_logp ? policy + (double)a.kl_coef * kl : policy);
+    a.sums[5] = __int_as_float((int)taken);
+    a.sums[6] = __int_as_float((int)left_out);
+    a.sums[7] = 0.0f;
+}
 // a term past the caches, to a block that may sit on another die, and there
 __device__ __forceinline__ void leave_term(Term *to, const Term &t)
 {
@@ -141,38 +152,52 @@ __device__ __forceinline__ void sum_here(const LossArgs &a)
 #pragma unroll
         for (int k = 0; k < 4; ++k) if (i + 64u * k < a.rows) t[k] = left_term(a.terms + i + 64u * k); else t[k].kind = TERM_NONE;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s.add(t[k], a.kl_coef);
+        for (int k = 0; k < 4; ++k) s.add(t[k]);
     }
-    s.join();
-    if (threadIdx.x == 0) s.put(a.sums);
+    const double mine = s.join();
+    put_sums(a, __shfl(mine, (int)sum_of_lane(), 64), s.taken, s.left_out);      // (sum_of_lane is its own inverse on 0..3)
 }
-__global__ __launch_bounds__(kBlock) void loss_sums_k(LossArgs a)
+// A block for every kTermBlock rows, all of whose terms it asks for at once.  The sums of the rows of earlier launches stand behind the parts.
+constexpr int kTermThreads = 512;
+__global__ __launch_bounds__(kTermThreads) void loss_sums_k(LossArgs a)
 {
-    __shared__ double lds[kWavesPerBlock][kLossSums];
+    constexpr int EACH = kTermBlock / kTermThreads, WAVES = kTermThreads / 64;
+    __shared__ double lds[WAVES][kLossSums];
+    const uint32_t first = blockIdx.x * kTermBlock + threadIdx.x, lane = threadIdx.x & 63u;
+    Term t[EACH];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) if (first + (uint32_t)(kTermThreads * k) < a.rows) t[k] = a.terms[first + (uint32_t)(kTermThreads * k)]; else t[k].kind = TERM_NONE;
     Sums s;
-    const uint32_t first = blockIdx.x * kTermBlock, end = a.rows - first < kTermBlock ? a.rows : first + kTermBlock;
-    for (uint32_t i = first + threadIdx.x; i < end; i += kBlock * 4u) {
-        Term t[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) if (i + kBlock * k < end) t[k] = a.terms[i + kBlock * k]; else t[k].kind = TERM_NONE;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) s.add(t[k], a.kl_coef);
-    }
-    s.join();
-    if ((threadIdx.x & 63u) == 0)
-#pragma unroll
-        for (int k = 0; k < kLossSums; ++k) lds[threadIdx.x >> 6][k] = s.at[k];
+    for (int k = 0; k < EACH; ++k) s.add(t[k]);
+    const double mine = s.join();
+    double *w = lds[threadIdx.x >> 6];
+    if (lane < 4u) w[sum_of_lane()] = mine;
+    if (lane == 0) { w[4] = (double)s.taken; w[5] = (double)s.left_out; }
     __syncthreads();
     if (threadIdx.x >= 64u) return;
-    double *before = a.partial + (size_t)kLossSums * kLossPartials;
-    const uint32_t k = threadIdx.x;
-    if (k < (uint32_t)kLossSums) leave_sum(a.partial + (size_t)k * kLossPartials + blockIdx.x, (lds[0][k] + lds[1][k]) + (lds[2][k] + lds[3][k]));
-    if (!arrives_last(a.counts) || k >= (uint32_t)kLossSums) return;
-    double sum = a.more ? before[k] : 0.0;
-    for (uint32_t i = 0; i < gridDim.x; ++i) sum += left_sum(a.partial + (size_t)k * kLossPartials + i);
-    before[k] = sum;
-    a.sums[k] = k < 5u ? (float)sum : __int_as_float((int)sum);
-    if (k == 0) a.sums[kLossSums] = 0.0f;
+    const bool has = lane < (uint32_t)kLossSums;
+    double sum = 0.0;
+    if (has)
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) sum += lds[k][lane];
+    double *behind = a.partial + (size_t)kLossSums * kLossPartials;
+    if (gridDim.x > 1u) {
+        if (has) leave_sum(a.partial + (size_t)lane * kLossPartials + blockIdx.x, sum);
+        if (!arrives_last(a.counts)) return;
+        sum = 0.0;
+        for (uint32_t i = 0; has && i < gridDim.x; i += 16u) {
+            double x[16];
+#pragma unroll
+            for (uint32_t k = 0; k < 16u; ++k) x[k] = i + k < gridDim.x ? left_sum(a.partial + (size_t)lane * kLossPartials + i + k) : 0.0;
+#pragma unroll
+            for (uint32_t k = 0; k < 16u; ++k) sum += x[k];
+        }
+    }
+    if (has && a.more) sum += behind[lane];
+    if (has) behind[lane] = sum;
+    const uint32_t taken = (uint32_t)__shfl(sum, 4, 64), left_out = (uint32_t)__shfl(sum, 5, 64);
+    put_sums(a, sum, taken, left_out);
 }
 
 // ---- rows that fit the registers of those who share them ----------------------------------------------------------------
@@ -612,9 +637,10 @@ static uint32_t reach(const LossArgs &a, uint32_t line)
     return (uint32_t)((shift / sizeof(T) + a.vocab) / Raw<T>::N);
 }
 // At most kTermRows rows; whether their terms are added up.
-// Threads to a row: as few as hold it in the registers that let 32 wavefronts share a compute unit (64), up to 65536 elements of 16 bits; of longer
-// rows twice that.  Rates of the policy loss in bf16 (TB/s): 4096 x 32064 5.4, 32003 (rows begin anywhere) 5.4, both with one row in eight masked; with 40 %
-// masked 4096 x 32064 5.2, 8192 x 8192 4.7, 16384 x 4096 4.9, 32768 x 1000 3.6, 65536 x 100 1.2, 2048 x 65536 5.0, 2048 x 128259 5.2, 1024 x 200001 4.9.
+// Threads to a row: few enough for several rows to a wavefront where rows are short (32768 x 200 / 500 / 1000 bf16 with 16, 32 and 64 threads to a row: 12.9 /
+// 21.5 / 27.9, 15.2 / 19.8 / 31.1 and 19.7 / 22.2 / 27.7 us), else as few as hold it in the registers that let 32 wavefronts share a compute unit (64), up to 65536 elements of 16 bits; of longer
+// rows twice that.  Rates of the policy loss in bf16 (TB/s): 4096 x 32064 5.5, 32003 (rows begin anywhere) 5.5, both with one row in eight masked; with 40 %
+// masked 4096 x 32064 5.3, 8192 x 8192 4.9, 16384 x 4096 5.1, 32768 x 1000 3.9, 65536 x 100 1.4, 2048 x 65536 5.1, 2048 x 128259 5.3, 1024 x 200001 5.0.
 template <class T, bool LOSS>
 static bool loss_of(const LaunchCtx &lc, LossArgs a)
 {
@@ -622,7 +648,7 @@ static bool loss_of(const LaunchCtx &lc, LossArgs a)
     // (a row that would need twice the registers for it is not moved to a line)
     const uint32_t close = reach<T>(a, 16u);
     uint32_t vecs = reach<T>(a, kLine);
-    for (uint32_t room : {16u, 64u, 128u, 256u, 512u, 1024u, 2048u, 4096u, 8192u, 16384u}) if (close <= room && room < vecs) { a.line = 16u; vecs = close; }
+    for (uint32_t room : {16u, 32u, 64u, 128u, 256u, 512u, 1024u, 2048u, 4096u, 8192u, 16384u}) if (close <= room && room < vecs) { a.line = 16u; vecs = close; }
     // Few long rows are shared by blocks.  (Policy loss so and with a block to each, us: rows of 128256 bf16, 1 / 64 / 128 / 200 of them 13.6 / 14.0 / 19.0 / 27.5
     // and 18.2 / 21.0 / 21.7 / 23.7; of 262144 fp32 13.6 / 30.8 / 56.9 / 88.3 and 42.9 / 51.6 / 71.0 / 97.0; of 70000 bf16, 64 / 128 / 200 13.1 / 15.1 / 17.6 and
     // 17.1 / 17.6 / 18.3.  Below 8192 vectors the second launch costs more than it gains: 1 / 64 of 64000 bf16 13.5 / 13.3 and 11.8 / 14.0, their
@@ -635,7 +661,8 @@ static bool loss_of(const LaunchCtx &lc, LossArgs a)
         return LOSS;
     }
     if (vecs <= 16 * 1) return held<T, 16, 1, true, LOSS>(lc, a);
-    if (vecs <= 64 * 1) return held<T, 64, 1, true, LOSS>(lc, a);
+    if (vecs <= 16 * 2) return held<T, 16, 2, true, LOSS>(lc, a);
+    if (vecs <= 32 * 2) return held<T, 32, 2, true, LOSS>(lc, a);
     if (vecs <= 64 * 2) return held<T, 64, 2, true, LOSS>(lc, a);
     if (vecs <= 64 * 4) return held<T, 64, 4, true, LOSS>(lc, a);
     if (vecs <= 256 * 2) return held<T, 256, 2, true, LOSS>(lc, a);
@@ -650,7 +677,7 @@ static bool loss_of(const LaunchCtx &lc, LossArgs a)
     return here;
 }
 // the sums of no rows
-__global__ void no_rows_k(float *sums) { if (threadIdx.x <= (uint32_t)kLossSums) sums[threadIdx.x] = 0.0f; }
+__global__ void no_rows_k(float *sums) { if (threadIdx.x < 8u) sums[threadIdx.x] = 0.0f; }
 
 template <bool LOSS>
 static void loss_by(const LaunchCtx &lc, int dtype, LossArgs a)
@@ -659,7 +686,7 @@ static void loss_by(const LaunchCtx &lc, int dtype, LossArgs a)
     for (uint32_t left = a.rows; left;) {
         a.rows = left < kTermRows ? left : kTermRows;
         const bool done = dtype == MC_DTYPE_F32 ? loss_of<float, LOSS>(lc, a) : dtype == MC_DTYPE_BF16 ? loss_of<__bf16, LOSS>(lc, a) : loss_of<_Float16, LOSS>(lc, a);
-        if (LOSS && !done) launch(loss_sums_k, dim3((a.rows + kTermBlock - 1) / kTermBlock), dim3(kBlock), lc.stream, a);
+        if (LOSS && !done) launch(loss_sums_k, dim3((a.rows + kTermBlock - 1) / kTermBlock), dim3(kTermThreads), lc.stream, a);
         left -= a.rows;
         a.more = true;
         a.logits = static_cast<const char *>(a.logits) + (int64_t)a.rows * a.stride * size;

@@ -41,7 +41,7 @@ void launch_grad_clip(const LaunchCtx &lc, int dtype, const StepView &v, uint32_
 void launch_adamw(const LaunchCtx &lc, int dtype, int model_dtype, const StepView &v, const AdamwArgs &a);
 
 // ---- rows of logits -----------------------------------------------------------------------------------------------
-constexpr int kLossSums = 7;                 // five sums and two counts
+constexpr int kLossSums = 6;                 // four sums and two counts
 // What a row adds to them.
 struct alignas(16) Term {
     float policy, kl, weight;
@@ -49,7 +49,7 @@ struct alignas(16) Term {
 };
 enum TermKind { TERM_NONE = 0, TERM_FREE = 1, TERM_CUT = 2, TERM_LEFT_OUT = 3 };      // takes no part; does; does and the clamp decides; has a weight, but no valid label
 constexpr uint32_t kTermRows = 1u << 17;     // rows that there is room for: more of them are taken so many at a time
-constexpr uint32_t kTermBlock = 4096;        // rows per block of the kernel that adds them up
+constexpr uint32_t kTermBlock = 2048;        // rows per block of the kernel that adds them up
 constexpr uint32_t kLossPartials = kTermRows / kTermBlock;
 // The parts of a row that several blocks share.
 constexpr uint32_t kPartRows = 128, kMostParts = 64;
