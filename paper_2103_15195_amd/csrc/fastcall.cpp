@@ -1,4 +1,4 @@
-// The hot calls of the binding without ctypes: a small call's launch takes the host 2.6 us, and what ctypes and the Python
+// The hot calls of the bindings without ctypes: a small call's launch takes the host 2.6 us, and what ctypes and the Python
 // around it took to bring its arguments there nearly as long again.
 // Each function takes the arguments in the forms that a hot loop passes -- Python ints, a float, ctypes arrays of addresses, tensors, no
 // stream -- and returns the library's status; for anything else it returns None and has done nothing, and the caller takes the ctypes route, which
@@ -199,9 +199,170 @@ void raw_stream_gone(PyObject *self)
     Py_TYPE(self)->tp_free(self);
 }
 
+// ---- rows of logits (step.py) -----------------------------------------------------------------------------------------
+// The structures of mergecomp_step.h.
+struct Logits {
+    const void *logits, *labels;
+    int64_t rows, vocab, stride;
+    int32_t dtype;
+    float temperature;
+};
+struct Policy {
+    const void *old_logp, *advantages, *weights, *ref_logp;
+    float clip_low, clip_high, kl_coef, grad_scale;
+    void *sums, *logp, *dlogits;
+    int64_t dlogits_stride;
+};
+typedef int (*token_logp_fn)(void *, const Logits *, void *, void *);
+typedef int (*policy_loss_fn)(void *, const Logits *, const Policy *, void *);
+
+PyObject *g_dtype, *g_is_cuda, *g_shape, *g_stride;      // names
+
+// The entry points over rows of logits, and torch's types: of logits by their numbers there, and of labels.
+struct RowCalls {
+    PyObject_HEAD
+    PyObject *kinds[3], *int64;
+    token_logp_fn token_logp;
+    policy_loss_fn policy_loss;
+};
+bool is_true(PyObject *o, PyObject *name)
+{
+    PyObject *x = PyObject_GetAttr(o, name);
+    Py_XDECREF(x);                    // (a bool: the interpreter's own)
+    return x == Py_True;
+}
+// whether the tensor's type is `kind`
+bool of_kind(PyObject *o, PyObject *kind)
+{
+    PyObject *x = PyObject_GetAttr(o, g_dtype);
+    Py_XDECREF(x);                    // (torch's types live as long as torch)
+    return x && x == kind;
+}
+// sizes and strides of a tensor of n dimensions
+bool layout(PyObject *o, int n, int64_t *size, int64_t *step)
+{
+    PyObject *shape = PyObject_GetAttr(o, g_shape), *stride = shape ? PyObject_CallMethodNoArgs(o, g_stride) : nullptr;
+    bool ok = shape && stride && PyTuple_Check(shape) && PyTuple_Check(stride) && PyTuple_GET_SIZE(shape) == n && PyTuple_GET_SIZE(stride) == n;
+    for (int i = 0; ok && i < n; ++i) {
+        size[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i));
+        step[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(stride, i));
+        ok = !PyErr_Occurred();
+    }
+    Py_XDECREF(shape);
+    Py_XDECREF(stride);
+    return ok;
+}
+// a device tensor of one dimension, `count` contiguous elements of a type; None only where allowed
+bool vector(PyObject *o, int64_t count, PyObject *kind, const void **p, bool optional = false)
+{
+    *p = nullptr;
+    if (o == Py_None) return optional;
+    int64_t size, step;
+    void *at;
+    if (!of_kind(o, kind) || !is_true(o, g_is_cuda) || !layout(o, 1, &size, &step) || size != count || (step != 1 && size > 1) || !tensor(o, &at)) return false;
+    *p = at;
+    return true;
+}
+// rows of contiguous elements: their type's number, or -1
+int matrix(const RowCalls *c, PyObject *o, int64_t *size, int64_t *stride, void **p)
+{
+    int64_t step[2];
+    PyObject *kind = PyObject_GetAttr(o, g_dtype);
+    int k = 0;
+    while (k < 3 && c->kinds[k] != kind) ++k;
+    Py_XDECREF(kind);
+    if (!kind || k == 3 || !is_true(o, g_is_cuda) || !layout(o, 2, size, step) || (step[1] != 1 && size[1] > 1) || !tensor(o, p)) return -1;
+    *stride = size[0] > 1 || step[0] > size[1] ? step[0] : size[1];
+    return k;
+}
+bool number(PyObject *o, float *f)
+{
+    if (!PyFloat_CheckExact(o)) return false;
+    *f = (float)PyFloat_AS_DOUBLE(o);
+    return true;
+}
+bool logits_of(const RowCalls *c, PyObject *logits, PyObject *labels, PyObject *temperature, Logits *x)
+{
+    int64_t size[2];
+    void *at;
+    x->dtype = matrix(c, logits, size, &x->stride, &at);
+    if (x->dtype < 0) return false;
+    x->logits = at;
+    x->rows = size[0];
+    x->vocab = size[1];
+    return vector(labels, size[0], c->int64, &x->labels) && number(temperature, &x->temperature);
+}
+// (handle, logits, labels, log-probabilities, temperature, the stream's callable)
+PyObject *token_logp(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const RowCalls *c = reinterpret_cast<const RowCalls *>(self);
+    void *handle, *stream;
+    const void *logp;
+    Logits x;
+    if (n != 6 || !address(a[0], &handle) || !logits_of(c, a[1], a[2], a[4], &x) || !vector(a[3], x.rows, c->kinds[0], &logp) || !stream_of(a[5], &stream)) return other();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = c->token_logp(handle, &x, const_cast<void *>(logp), stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+// (handle, logits, labels, old_logp, advantages, weights, ref_logp, clip_low, clip_high, kl_coef, temperature, grad_scale, sums, logp, dlogits, the
+// stream's callable)
+PyObject *policy_loss(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const RowCalls *c = reinterpret_cast<const RowCalls *>(self);
+    void *handle, *stream;
+    const void *sums, *logp;
+    Logits x;
+    Policy p;
+    PyObject *f32 = c->kinds[0];
+    if (n != 16 || !address(a[0], &handle) || !logits_of(c, a[1], a[2], a[10], &x) || !vector(a[3], x.rows, f32, &p.old_logp) ||
+        !vector(a[4], x.rows, f32, &p.advantages) || !vector(a[5], x.rows, f32, &p.weights, true) || !vector(a[6], x.rows, f32, &p.ref_logp, true) ||
+        !number(a[7], &p.clip_low) || !number(a[8], &p.clip_high) || !number(a[9], &p.kl_coef) || !number(a[11], &p.grad_scale) ||
+        !vector(a[12], 8, f32, &sums) || !vector(a[13], x.rows, f32, &logp, true)) return other();
+    p.sums = const_cast<void *>(sums);
+    p.logp = const_cast<void *>(logp);
+    p.dlogits = nullptr;
+    p.dlogits_stride = 0;
+    if (a[14] != Py_None) {
+        int64_t size[2];
+        if (matrix(c, a[14], size, &p.dlogits_stride, &p.dlogits) != x.dtype || size[0] != x.rows || size[1] != x.vocab) return other();
+    }
+    if (!stream_of(a[15], &stream)) return other();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = c->policy_loss(handle, &x, &p, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+// RowCalls(float32, bfloat16, float16, int64, addresses of mc_token_logp, mc_policy_loss)
+PyObject *row_calls_new(PyTypeObject *type, PyObject *args, PyObject *)
+{
+    PyObject *kinds[4] = {};
+    unsigned long long at[2] = {};
+    if (!PyArg_ParseTuple(args, "OOOOKK", &kinds[0], &kinds[1], &kinds[2], &kinds[3], &at[0], &at[1])) return nullptr;
+    RowCalls *c = reinterpret_cast<RowCalls *>(type->tp_alloc(type, 0));
+    if (!c) return nullptr;
+    for (PyObject *k : kinds) Py_INCREF(k);
+    for (int k = 0; k < 3; ++k) c->kinds[k] = kinds[k];
+    c->int64 = kinds[3];
+    c->token_logp = (token_logp_fn)(uintptr_t)at[0];
+    c->policy_loss = (policy_loss_fn)(uintptr_t)at[1];
+    return reinterpret_cast<PyObject *>(c);
+}
+void row_calls_gone(PyObject *self)
+{
+    RowCalls *c = reinterpret_cast<RowCalls *>(self);
+    for (PyObject *k : c->kinds) Py_XDECREF(k);
+    Py_XDECREF(c->int64);
+    Py_TYPE(self)->tp_free(self);
+}
+
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef calls_methods[] = {FAST(compress), FAST(compress_static), FAST(decompress), FAST(compress_groups), FAST(decompress_groups), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef row_calls_methods[] = {FAST(token_logp), FAST(policy_loss), {nullptr, nullptr, 0, nullptr}};
 PyTypeObject CallsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
+PyTypeObject RowCallsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 PyTypeObject RawStreamType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", "The hot calls of the binding without ctypes.", -1, nullptr, nullptr, nullptr, nullptr, nullptr};
 
@@ -209,7 +370,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", "The hot calls of the 
 
 PyMODINIT_FUNC PyInit__fastcall(void)
 {
-    if (!g_data_ptr && !(g_data_ptr = PyUnicode_InternFromString("data_ptr"))) return nullptr;
+    const struct { PyObject **at; const char *name; } names[] = {{&g_data_ptr, "data_ptr"}, {&g_dtype, "dtype"}, {&g_is_cuda, "is_cuda"}, {&g_shape, "shape"}, {&g_stride, "stride"}};
+    for (const auto &n : names) if (!*n.at && !(*n.at = PyUnicode_InternFromString(n.name))) return nullptr;
     CallsType.tp_name = "_fastcall.Calls";
     CallsType.tp_basicsize = sizeof(Calls);
     CallsType.tp_flags = Py_TPFLAGS_DEFAULT;
@@ -222,10 +384,17 @@ PyMODINIT_FUNC PyInit__fastcall(void)
     RawStreamType.tp_new = raw_stream_new;
     RawStreamType.tp_dealloc = raw_stream_gone;
     RawStreamType.tp_call = raw_stream_call;
-    if (PyType_Ready(&CallsType) < 0 || PyType_Ready(&RawStreamType) < 0) return nullptr;
+    RowCallsType.tp_name = "_fastcall.RowCalls";
+    RowCallsType.tp_basicsize = sizeof(RowCalls);
+    RowCallsType.tp_flags = Py_TPFLAGS_DEFAULT;
+    RowCallsType.tp_new = row_calls_new;
+    RowCallsType.tp_dealloc = row_calls_gone;
+    RowCallsType.tp_methods = row_calls_methods;
+    if (PyType_Ready(&CallsType) < 0 || PyType_Ready(&RawStreamType) < 0 || PyType_Ready(&RowCallsType) < 0) return nullptr;
     PyObject *m = PyModule_Create(&module);
     if (!m) return nullptr;
     if (PyModule_AddObjectRef(m, "Calls", reinterpret_cast<PyObject *>(&CallsType)) < 0 ||
+        PyModule_AddObjectRef(m, "RowCalls", reinterpret_cast<PyObject *>(&RowCallsType)) < 0 ||
         PyModule_AddObjectRef(m, "RawStream", reinterpret_cast<PyObject *>(&RawStreamType)) < 0) { Py_DECREF(m); return nullptr; }
     return m;
 }

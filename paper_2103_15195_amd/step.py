@@ -57,8 +57,22 @@ def lib():
         L.mc_loss_destroy.argtypes = [vp]
         L.mc_token_logp.argtypes = [vp, C.POINTER(McLogits), vp, vp]
         L.mc_policy_loss.argtypes = [vp, C.POINTER(McLogits), C.POINTER(McPolicy), vp]
+        try:
+            L.fast_rows = B._fastcall().RowCalls(torch.float32, torch.bfloat16, torch.float16, torch.int64,
+                                                 *[C.cast(f, vp).value for f in (L.mc_token_logp, L.mc_policy_loss)])
+        except ImportError:                      # (the library's own loading has warned)
+            L.fast_rows = _NoFastRows()
         _declared = L
     return L
+
+
+class _NoFastRows:
+    """Stands for the extension module's calls where there is no module: no argument is in a form that it takes."""
+
+    @staticmethod
+    def token_logp(*args):
+        return None
+    policy_loss = token_logp
 
 
 def dtype_id(dtype) -> int:
@@ -163,12 +177,16 @@ class PolicyLoss:
 
     def __init__(self):
         self._h = C.c_void_p()
+        self._at = 0                             # the same as an int
         B._check(lib().mc_loss_create(C.byref(self._h)), "mc_loss_create")
+        self._at = self._h.value
+        self._fast = lib().fast_rows
 
     def close(self) -> None:
         if getattr(self, "_h", None):
             lib().mc_loss_destroy(self._h)
             self._h = None
+            self._at = 0
 
     def __del__(self):
         try:
@@ -178,9 +196,11 @@ class PolicyLoss:
 
     def mc_token_logp(self, logits, labels, logp, temperature: float = 1.0, stream=None) -> None:
         """logp[r] = log-probability of labels[r] under logits[r] / temperature; 0 where the label is none of the row's."""
-        rows, vocab, stride = _rows(logits, "logits")
-        x = McLogits(logits.data_ptr(), _vector(labels, "labels", rows, _I64), rows, vocab, stride, DTYPE_IDS[logits.dtype], temperature)
-        rc = lib().mc_token_logp(self._h, C.byref(x), _vector(logp, "logp", rows), B._stream_handle(stream))
+        rc = self._fast.token_logp(self._at, logits, labels, logp, temperature, B._raw_stream) if stream is None else None
+        if rc is None:
+            rows, vocab, stride = _rows(logits, "logits")
+            x = McLogits(logits.data_ptr(), _vector(labels, "labels", rows, _I64), rows, vocab, stride, DTYPE_IDS[logits.dtype], temperature)
+            rc = lib().mc_token_logp(self._h, C.byref(x), _vector(logp, "logp", rows), B._stream_handle(stream))
         if rc:
             raise B.McError(rc, "mc_token_logp")
 
@@ -189,6 +209,16 @@ class PolicyLoss:
         """The loss of mergecomp_step.h and, in dlogits (which may be the logits), grad_scale times its gradient.
         sums: 8 floats on the device: loss, policy term, KL term, clipped weight, weight; as int32 rows that took part, rows
         whose label is none of the row's; 0."""
+        rc = self._fast.policy_loss(self._at, logits, labels, old_logp, advantages, weights, ref_logp, clip[0], clip[1], kl_coef, temperature,
+                                    grad_scale, sums, logp, dlogits, B._raw_stream) if stream is None else None
+        if rc is None:
+            rc = self._policy_loss(logits, labels, old_logp, advantages, sums, weights, ref_logp, clip, kl_coef, temperature, grad_scale, logp,
+                                   dlogits, B._stream_handle(stream))
+        if rc:
+            raise B.McError(rc, "mc_policy_loss")
+
+    def _policy_loss(self, logits, labels, old_logp, advantages, sums, weights, ref_logp, clip, kl_coef, temperature, grad_scale, logp, dlogits, stream) -> int:
+        """The same through ctypes, which says what is wrong with an argument."""
         rows, vocab, stride = _rows(logits, "logits")
         x = McLogits(logits.data_ptr(), _vector(labels, "labels", rows, _I64), rows, vocab, stride, DTYPE_IDS[logits.dtype], temperature)
         slopes, dstride = None, 0
@@ -200,6 +230,4 @@ class PolicyLoss:
         p = McPolicy(_vector(old_logp, "old_logp", rows), _vector(advantages, "advantages", rows),
                      None if weights is None else _vector(weights, "weights", rows), None if ref_logp is None else _vector(ref_logp, "ref_logp", rows),
                      clip[0], clip[1], kl_coef, grad_scale, _vector(sums, "sums", 8), None if logp is None else _vector(logp, "logp", rows), slopes, dstride)
-        rc = lib().mc_policy_loss(self._h, C.byref(x), C.byref(p), B._stream_handle(stream))
-        if rc:
-            raise B.McError(rc, "mc_policy_loss")
+        return lib().mc_policy_loss(self._h, C.byref(x), C.byref(p), stream)
