@@ -72,11 +72,12 @@ int mc_step_bind(mc_step *h, int32_t list, const void *const *ptrs, void *stream
 
 /*
  * norm = scale * sqrt(sum of the squares of all elements of all gradients)
- * coef = scale * min(1, max_norm / (norm + 1e-6)), or 0 if the norm is not a number or infinite
+ * coef = scale * min(1, max_norm / (norm + 1e-6)), or 0 if a gradient holds an infinity or a NaN
  *   scale      what a gradient is multiplied by before anything else (1 / loss scale, 1 / accumulated steps); finite, > 0
  *   max_norm   > 0; infinity: nothing is clipped
  *   out        device, two floats: norm, coef
- * Squares are summed in binary64, so that neither large nor small gradients are lost.
+ * Squares are summed in binary64, so that neither large nor small gradients are lost.  (A finite norm beyond binary32 is
+ * written as infinity; its coef is right.)
  */
 int mc_grad_norm(mc_step *h, float scale, float max_norm, float *out, void *stream);
 

@@ -236,6 +236,7 @@ static int logits_args(const mc_loss *h, const mc_logits *x, LossArgs &a)
     a.vocab = (uint32_t)x->vocab;
     const double base2 = 1.4426950408889634 / (double)x->temperature;
     a.to_base2 = (float)base2;
+    if (!std::isfinite(a.to_base2)) return MC_ERR_INVALID_ARG;          // (a temperature below 4.3e-39)
     a.to_base2_rest = (float)(base2 - (double)a.to_base2);
     a.inv_t = 1.0 / (double)x->temperature;
     a.partial = h->d_partial;
@@ -272,6 +273,7 @@ int mc_policy_loss(mc_loss *h, const mc_logits *x, const mc_policy *p, void *str
     a.sums = p->sums; a.logp = p->logp; a.dlogits = p->dlogits; a.dstride = p->dlogits_stride;
     a.lo = 1.0f - p->clip_low; a.hi = 1.0f + p->clip_high; a.kl_coef = p->kl_coef;
     a.gscale = (float)((double)p->grad_scale / (double)x->temperature);
+    if (!std::isfinite(a.gscale)) return MC_ERR_INVALID_ARG;
     launch_policy_loss(on(stream), x->dtype, a);
     return launched();
 }
