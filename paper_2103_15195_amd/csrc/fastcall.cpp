@@ -199,7 +199,7 @@ void raw_stream_gone(PyObject *self)
     Py_TYPE(self)->tp_free(self);
 }
 
-// ---- rows of logits (step.py) -----------------------------------------------------------------------------------------
+// ---- lists of tensors and rows of logits (step.py) -----------------------------------------------------------------------------------------
 // The structures of mergecomp_step.h.
 struct Logits {
     const void *logits, *labels;
@@ -213,17 +213,25 @@ struct Policy {
     void *sums, *logp, *dlogits;
     int64_t dlogits_stride;
 };
+struct Adamw {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;
+};
+typedef int (*grad_norm_fn)(void *, float, float, void *, void *);
+typedef int (*adamw_fn)(void *, const Adamw *, const void *, void *);
 typedef int (*token_logp_fn)(void *, const Logits *, void *, void *);
 typedef int (*policy_loss_fn)(void *, const Logits *, const Policy *, void *);
 
 PyObject *g_dtype, *g_is_cuda, *g_shape, *g_stride;      // names
 
-// The entry points over rows of logits, and torch's types: of logits by their numbers there, and of labels.
-struct RowCalls {
+// The entry points, and torch's types: of values by their numbers there, and of labels.
+struct StepCalls {
     PyObject_HEAD
     PyObject *kinds[3], *int64;
     token_logp_fn token_logp;
     policy_loss_fn policy_loss;
+    grad_norm_fn grad_norm, grad_clip;
+    adamw_fn adamw;
 };
 bool is_true(PyObject *o, PyObject *name)
 {
@@ -264,7 +272,7 @@ bool vector(PyObject *o, int64_t count, PyObject *kind, const void **p, bool opt
     return true;
 }
 // rows of contiguous elements: their type's number, or -1
-int matrix(const RowCalls *c, PyObject *o, int64_t *size, int64_t *stride, void **p)
+int matrix(const StepCalls *c, PyObject *o, int64_t *size, int64_t *stride, void **p)
 {
     int64_t step[2];
     PyObject *kind = PyObject_GetAttr(o, g_dtype);
@@ -281,7 +289,7 @@ bool number(PyObject *o, float *f)
     *f = (float)PyFloat_AS_DOUBLE(o);
     return true;
 }
-bool logits_of(const RowCalls *c, PyObject *logits, PyObject *labels, PyObject *temperature, Logits *x)
+bool logits_of(const StepCalls *c, PyObject *logits, PyObject *labels, PyObject *temperature, Logits *x)
 {
     int64_t size[2];
     void *at;
@@ -295,7 +303,7 @@ bool logits_of(const RowCalls *c, PyObject *logits, PyObject *labels, PyObject *
 // (handle, logits, labels, log-probabilities, temperature, the stream's callable)
 PyObject *token_logp(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
-    const RowCalls *c = reinterpret_cast<const RowCalls *>(self);
+    const StepCalls *c = reinterpret_cast<const StepCalls *>(self);
     void *handle, *stream;
     const void *logp;
     Logits x;
@@ -310,7 +318,7 @@ PyObject *token_logp(PyObject *self, PyObject *const *a, Py_ssize_t n)
 // stream's callable)
 PyObject *policy_loss(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
-    const RowCalls *c = reinterpret_cast<const RowCalls *>(self);
+    const StepCalls *c = reinterpret_cast<const StepCalls *>(self);
     void *handle, *stream;
     const void *sums, *logp;
     Logits x;
@@ -335,24 +343,65 @@ PyObject *policy_loss(PyObject *self, PyObject *const *a, Py_ssize_t n)
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
 }
-// RowCalls(float32, bfloat16, float16, int64, addresses of mc_token_logp, mc_policy_loss)
-PyObject *row_calls_new(PyTypeObject *type, PyObject *args, PyObject *)
+// (handle, scale, max_norm, the record, the stream's callable)
+PyObject *norm_by(PyObject *self, PyObject *const *a, Py_ssize_t n, bool clip)
+{
+    const StepCalls *c = reinterpret_cast<const StepCalls *>(self);
+    void *handle, *stream;
+    const void *out;
+    float scale, most;
+    if (n != 5 || !address(a[0], &handle) || !number(a[1], &scale) || !number(a[2], &most) || !vector(a[3], 2, c->kinds[0], &out) || !stream_of(a[4], &stream)) return other();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = (clip ? c->grad_clip : c->grad_norm)(handle, scale, most, const_cast<void *>(out), stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+PyObject *grad_norm(PyObject *self, PyObject *const *a, Py_ssize_t n) { return norm_by(self, a, n, false); }
+PyObject *grad_clip(PyObject *self, PyObject *const *a, Py_ssize_t n) { return norm_by(self, a, n, true); }
+// (handle, step, lr, beta1, beta2, eps, weight_decay, coefficient or None, the stream's callable)
+PyObject *adamw(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const StepCalls *c = reinterpret_cast<const StepCalls *>(self);
+    void *handle, *stream;
+    const void *coef;
+    Adamw w;
+    double *const at[] = {&w.lr, &w.beta1, &w.beta2, &w.eps, &w.weight_decay};
+    if (n != 9 || !address(a[0], &handle) || !PyLong_Check(a[1])) return other();
+    w.step = PyLong_AsLongLong(a[1]);
+    if (w.step == -1 && PyErr_Occurred()) return other();
+    for (int k = 0; k < 5; ++k) {
+        if (!PyFloat_CheckExact(a[2 + k])) return other();
+        *at[k] = PyFloat_AS_DOUBLE(a[2 + k]);
+    }
+    if (!vector(a[7], 1, c->kinds[0], &coef, true) || !stream_of(a[8], &stream)) return other();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = c->adamw(handle, &w, coef, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+// StepCalls(float32, bfloat16, float16, int64, addresses of mc_token_logp, mc_policy_loss, mc_grad_norm, mc_grad_clip, mc_adamw)
+PyObject *step_calls_new(PyTypeObject *type, PyObject *args, PyObject *)
 {
     PyObject *kinds[4] = {};
-    unsigned long long at[2] = {};
-    if (!PyArg_ParseTuple(args, "OOOOKK", &kinds[0], &kinds[1], &kinds[2], &kinds[3], &at[0], &at[1])) return nullptr;
-    RowCalls *c = reinterpret_cast<RowCalls *>(type->tp_alloc(type, 0));
+    unsigned long long at[5] = {};
+    if (!PyArg_ParseTuple(args, "OOOOKKKKK", &kinds[0], &kinds[1], &kinds[2], &kinds[3], &at[0], &at[1], &at[2], &at[3], &at[4])) return nullptr;
+    StepCalls *c = reinterpret_cast<StepCalls *>(type->tp_alloc(type, 0));
     if (!c) return nullptr;
     for (PyObject *k : kinds) Py_INCREF(k);
     for (int k = 0; k < 3; ++k) c->kinds[k] = kinds[k];
     c->int64 = kinds[3];
     c->token_logp = (token_logp_fn)(uintptr_t)at[0];
     c->policy_loss = (policy_loss_fn)(uintptr_t)at[1];
+    c->grad_norm = (grad_norm_fn)(uintptr_t)at[2];
+    c->grad_clip = (grad_norm_fn)(uintptr_t)at[3];
+    c->adamw = (adamw_fn)(uintptr_t)at[4];
     return reinterpret_cast<PyObject *>(c);
 }
-void row_calls_gone(PyObject *self)
+void step_calls_gone(PyObject *self)
 {
-    RowCalls *c = reinterpret_cast<RowCalls *>(self);
+    StepCalls *c = reinterpret_cast<StepCalls *>(self);
     for (PyObject *k : c->kinds) Py_XDECREF(k);
     Py_XDECREF(c->int64);
     Py_TYPE(self)->tp_free(self);
@@ -360,9 +409,9 @@ void row_calls_gone(PyObject *self)
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef calls_methods[] = {FAST(compress), FAST(compress_static), FAST(decompress), FAST(compress_groups), FAST(decompress_groups), {nullptr, nullptr, 0, nullptr}};
-PyMethodDef row_calls_methods[] = {FAST(token_logp), FAST(policy_loss), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef step_calls_methods[] = {FAST(token_logp), FAST(policy_loss), FAST(grad_norm), FAST(grad_clip), FAST(adamw), {nullptr, nullptr, 0, nullptr}};
 PyTypeObject CallsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
-PyTypeObject RowCallsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
+PyTypeObject StepCallsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 PyTypeObject RawStreamType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", "The hot calls of the binding without ctypes.", -1, nullptr, nullptr, nullptr, nullptr, nullptr};
 
@@ -384,17 +433,17 @@ PyMODINIT_FUNC PyInit__fastcall(void)
     RawStreamType.tp_new = raw_stream_new;
     RawStreamType.tp_dealloc = raw_stream_gone;
     RawStreamType.tp_call = raw_stream_call;
-    RowCallsType.tp_name = "_fastcall.RowCalls";
-    RowCallsType.tp_basicsize = sizeof(RowCalls);
-    RowCallsType.tp_flags = Py_TPFLAGS_DEFAULT;
-    RowCallsType.tp_new = row_calls_new;
-    RowCallsType.tp_dealloc = row_calls_gone;
-    RowCallsType.tp_methods = row_calls_methods;
-    if (PyType_Ready(&CallsType) < 0 || PyType_Ready(&RawStreamType) < 0 || PyType_Ready(&RowCallsType) < 0) return nullptr;
+    StepCallsType.tp_name = "_fastcall.StepCalls";
+    StepCallsType.tp_basicsize = sizeof(StepCalls);
+    StepCallsType.tp_flags = Py_TPFLAGS_DEFAULT;
+    StepCallsType.tp_new = step_calls_new;
+    StepCallsType.tp_dealloc = step_calls_gone;
+    StepCallsType.tp_methods = step_calls_methods;
+    if (PyType_Ready(&CallsType) < 0 || PyType_Ready(&RawStreamType) < 0 || PyType_Ready(&StepCallsType) < 0) return nullptr;
     PyObject *m = PyModule_Create(&module);
     if (!m) return nullptr;
     if (PyModule_AddObjectRef(m, "Calls", reinterpret_cast<PyObject *>(&CallsType)) < 0 ||
-        PyModule_AddObjectRef(m, "RowCalls", reinterpret_cast<PyObject *>(&RowCallsType)) < 0 ||
+        PyModule_AddObjectRef(m, "StepCalls", reinterpret_cast<PyObject *>(&StepCallsType)) < 0 ||
         PyModule_AddObjectRef(m, "RawStream", reinterpret_cast<PyObject *>(&RawStreamType)) < 0) { Py_DECREF(m); return nullptr; }
     return m;
 }

@@ -43,7 +43,7 @@ static void in_launches(StepView v, Body body)
 
 // ---- norm -----------------------------------------------------------------------------------------------------------
 // Squares are summed in binary64: of binary32 values they are exact there, and neither overflow nor vanish.  Blocks take pieces in
-// turn, and the last one to be done adds up what all have left: one launch (with the sums added up by a second one 7.0 instead of 5.0 us
+// turn, and the last one to be done adds up what all have left: one launch (with the sums added up by a second one 7.0 instead of 4.8 us
 // for 272 474 elements in 65 tensors).
 // 25.6 M elements in 161 tensors 19.3 us (5.3 TB/s), 120 M of 16 bits 43.0 (5.6 TB/s).  1024 blocks of 512 threads: of 256 threads 53.4 of
 // the latter, 2048 of 256 20.2 of the former and 43.4.
@@ -121,7 +121,7 @@ void launch_grad_clip(const LaunchCtx &lc, int dtype, const StepView &v, uint32_
 
 // ---- AdamW --------------------------------------------------------------------------------------------------------------
 // Four elements a thread: 16 bytes of each 32-bit list, 8 of a 16-bit one.  A block has a quarter of a piece and is done when its
-// one load of each list is: with the norm before it 25.6 M elements in 32 bits take 130 us, 160 M of mixed precision 769 (5.8 TB/s);
+// one load of each list is: with the norm before it 25.6 M elements in 32 bits take 130 us (5.5 TB/s), 160 M of mixed precision 770 (5.8 TB/s);
 // a block to a piece, four loads of each list a thread, 133 and 846.
 struct NoCopy {};
 constexpr uint32_t kAdamwSpan = kBlock * 4, kAdamwShares = kPiece / kAdamwSpan;
@@ -129,8 +129,7 @@ template <class T, class M>
 __global__ __launch_bounds__(kBlock) void adamw_k(StepView v, AdamwArgs a)
 {
     constexpr int N = 4;
-    const float coef = a.coef ? *a.coef : 1.0f;
-    if (coef == 0.0f) return;
+    const float coef = a.coef ? ld_uniform(a.coef) : 1.0f;
     const Span s = span_of<float>(v, blockIdx.x / kAdamwShares, MC_LIST_PARAMS);
     const global_ptr<const T> grad = span_in<const T>(v, MC_LIST_GRADS, s);
     const global_ptr<float> param = span_in<float>(v, MC_LIST_PARAMS, s), avg = span_in<float>(v, MC_LIST_EXP_AVG, s),
@@ -142,6 +141,7 @@ __global__ __launch_bounds__(kBlock) void adamw_k(StepView v, AdamwArgs a)
     load_some<N, float>(param, i, s.lo, s.hi, w);
     load_some<N, float>(avg, i, s.lo, s.hi, m);
     load_some<N, float>(avg_sq, i, s.lo, s.hi, q);
+    if (coef == 0.0f) return;            // (looked at behind the loads, which need not wait for it)
 #pragma unroll
     for (int e = 0; e < N; ++e) {
         g[e] *= coef;

@@ -58,21 +58,21 @@ def lib():
         L.mc_token_logp.argtypes = [vp, C.POINTER(McLogits), vp, vp]
         L.mc_policy_loss.argtypes = [vp, C.POINTER(McLogits), C.POINTER(McPolicy), vp]
         try:
-            L.fast_rows = B._fastcall().RowCalls(torch.float32, torch.bfloat16, torch.float16, torch.int64,
-                                                 *[C.cast(f, vp).value for f in (L.mc_token_logp, L.mc_policy_loss)])
+            L.fast_step = B._fastcall().StepCalls(torch.float32, torch.bfloat16, torch.float16, torch.int64, *[C.cast(f, vp).value for f in (
+                L.mc_token_logp, L.mc_policy_loss, L.mc_grad_norm, L.mc_grad_clip, L.mc_adamw)])
         except ImportError:                      # (the library's own loading has warned)
-            L.fast_rows = _NoFastRows()
+            L.fast_step = _NoFastCalls()
         _declared = L
     return L
 
 
-class _NoFastRows:
+class _NoFastCalls:
     """Stands for the extension module's calls where there is no module: no argument is in a form that it takes."""
 
     @staticmethod
     def token_logp(*args):
         return None
-    policy_loss = token_logp
+    policy_loss = grad_norm = grad_clip = adamw = token_logp
 
 
 def dtype_id(dtype) -> int:
@@ -122,14 +122,18 @@ class Step:
                        "params": MC_DTYPE_F32, "exp_avg": MC_DTYPE_F32, "exp_avg_sq": MC_DTYPE_F32}
         self._kept = {}
         self._h = C.c_void_p()
+        self._at = 0                             # the same as an int
         nm = (C.c_int64 * max(n, 1))(*self.numel)
         nd = None if no_decay is None else (C.c_uint8 * max(n, 1))(*[1 if x else 0 for x in no_decay])
         B._check(lib().mc_step_create(C.byref(self._h), nm, n, self.dtypes["grads"], self.dtypes["model"], nd), "mc_step_create")
+        self._at = self._h.value
+        self._fast = lib().fast_step
 
     def close(self) -> None:
         if getattr(self, "_h", None):
             lib().mc_step_destroy(self._h)
             self._h = None
+            self._at = 0
             self._kept = {}
 
     def __del__(self):
@@ -159,17 +163,29 @@ class Step:
 
     def mc_grad_norm(self, max_norm: float, out, scale: float = 1.0, stream=None) -> None:
         """out: two floats on the device, the norm of scale * gradients and the coefficient that clips them to max_norm."""
-        B._check(lib().mc_grad_norm(self._h, scale, max_norm, _vector(out, "out", 2), B._stream_handle(stream)), "mc_grad_norm")
+        rc = self._fast.grad_norm(self._at, scale, max_norm, out, B._raw_stream) if stream is None else None
+        if rc is None:
+            rc = lib().mc_grad_norm(self._h, scale, max_norm, _vector(out, "out", 2), B._stream_handle(stream))
+        if rc:
+            raise B.McError(rc, "mc_grad_norm")
 
     def mc_grad_clip(self, max_norm: float, out, scale: float = 1.0, stream=None) -> None:
         """mc_grad_norm, and the gradients times the coefficient into the list `clipped`, or in place where it is not bound."""
-        B._check(lib().mc_grad_clip(self._h, scale, max_norm, _vector(out, "out", 2), B._stream_handle(stream)), "mc_grad_clip")
+        rc = self._fast.grad_clip(self._at, scale, max_norm, out, B._raw_stream) if stream is None else None
+        if rc is None:
+            rc = lib().mc_grad_clip(self._h, scale, max_norm, _vector(out, "out", 2), B._stream_handle(stream))
+        if rc:
+            raise B.McError(rc, "mc_grad_clip")
 
     def mc_adamw(self, step: int, lr: float, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
                  coef=None, stream=None) -> None:
         """coef: one float on the device that the gradients are multiplied by, such as the second of mc_grad_norm."""
-        cfg = McAdamwConfig(lr, betas[0], betas[1], eps, weight_decay, step)
-        B._check(lib().mc_adamw(self._h, C.byref(cfg), None if coef is None else _vector(coef, "coef", 1), B._stream_handle(stream)), "mc_adamw")
+        rc = self._fast.adamw(self._at, step, lr, betas[0], betas[1], eps, weight_decay, coef, B._raw_stream) if stream is None else None
+        if rc is None:
+            cfg = McAdamwConfig(lr, betas[0], betas[1], eps, weight_decay, step)
+            rc = lib().mc_adamw(self._h, C.byref(cfg), None if coef is None else _vector(coef, "coef", 1), B._stream_handle(stream))
+        if rc:
+            raise B.McError(rc, "mc_adamw")
 
 
 class PolicyLoss:
@@ -180,7 +196,7 @@ class PolicyLoss:
         self._at = 0                             # the same as an int
         B._check(lib().mc_loss_create(C.byref(self._h)), "mc_loss_create")
         self._at = self._h.value
-        self._fast = lib().fast_rows
+        self._fast = lib().fast_step
 
     def close(self) -> None:
         if getattr(self, "_h", None):

@@ -1,4 +1,4 @@
-"""The extension module behind the calls over rows of logits, on functions that record what they are called with: arguments arrive
+"""The extension module behind the calls over lists of tensors and rows of logits, on functions that record what they are called with: arguments arrive
 in the header's structures, and what is not in a hot loop's form is left to ctypes (None, and no call)."""
 import ctypes as C
 
@@ -33,7 +33,10 @@ def calls():
     seen = []
     keep = [C.CFUNCTYPE(i32, vp, C.POINTER(S.McLogits), vp, vp)(lambda h, x, logp, st: seen.append((h, values(x[0]), logp, st)) or -7),
             C.CFUNCTYPE(i32, vp, C.POINTER(S.McLogits), C.POINTER(S.McPolicy), vp)(lambda h, x, p, st: seen.append((h, values(x[0]), values(p[0]), st)) or 3)]
-    fast = B._fastcall().RowCalls(torch.float32, torch.bfloat16, torch.float16, torch.int64, *[C.cast(k, vp).value for k in keep])
+    norm = C.CFUNCTYPE(i32, vp, C.c_float, C.c_float, vp, vp)
+    keep += [norm(lambda *a: seen.append(("norm", *a)) or -1), norm(lambda *a: seen.append(("clip", *a)) or -2),
+             C.CFUNCTYPE(i32, vp, C.POINTER(S.McAdamwConfig), vp, vp)(lambda h, c, coef, st: seen.append((h, values(c[0]), coef, st)) or 0)]
+    fast = B._fastcall().StepCalls(torch.float32, torch.bfloat16, torch.float16, torch.int64, *[C.cast(k, vp).value for k in keep])
     return fast, seen, keep
 
 
@@ -96,3 +99,21 @@ def test_other_forms_are_left_to_ctypes(calls):
     assert policy(fast, good(), at="8") is None and policy(fast, good(), stream=None) is None and policy(fast, good(), stream=lambda: None) is None
     assert fast.policy_loss(8) is None and fast.token_logp() is None
     assert not seen
+
+
+def test_lists(calls):
+    fast, seen, _ = calls
+    out, one = Tensor(64, (2,)), Tensor(80, (1,))
+    assert fast.grad_norm(8, 0.5, 2.0, out, stream) == -1 and seen[-1] == ("norm", 8, 0.5, 2.0, 64, 0x7000)
+    assert fast.grad_clip(8, 0.5, float("inf"), out, stream) == -2 and seen[-1] == ("clip", 8, 0.5, float("inf"), 64, 0x7000)
+    cfg = dict(lr=0.1, beta1=0.2, beta2=0.3, eps=0.4, weight_decay=0.5, step=2 ** 40)
+    assert fast.adamw(8, 2 ** 40, 0.1, 0.2, 0.3, 0.4, 0.5, one, stream) == 0 and seen[-1] == (8, cfg, 80, 0x7000)
+    assert fast.adamw(8, 2 ** 40, 0.1, 0.2, 0.3, 0.4, 0.5, None, stream) == 0 and seen[-1] == (8, cfg, None, 0x7000)
+    before = len(seen)
+    for bad in ((8, 1, 2.0, out, stream), (8, 0.5, None, out, stream), (8, 0.5, 2.0, one, stream), (8, 0.5, 2.0, None, stream), (8, 0.5, 2.0, out, None),
+                (8, 0.5, 2.0, Tensor(64, (2,), torch.float64), stream), (None, 0.5, 2.0, out, stream), (8, 0.5)):
+        assert fast.grad_norm(*bad) is None and fast.grad_clip(*bad) is None, bad
+    for bad in ((8, 1.0, 0.1, 0.2, 0.3, 0.4, 0.5, one, stream), (8, 2 ** 70, 0.1, 0.2, 0.3, 0.4, 0.5, one, stream), (8, 1, 0.1, 0.2, 0.3, 0.4, 0, one, stream),
+                (8, 1, 0.1, 0.2, 0.3, 0.4, 0.5, out, stream), (8, 1, 0.1, 0.2, 0.3, 0.4, 0.5, one, None), (8, 1)):
+        assert fast.adamw(*bad) is None, bad
+    assert len(seen) == before
