@@ -41,7 +41,8 @@ typedef struct mc_step mc_step;
 /* The lists that a handle knows, each one tensor for every tensor of the model. */
 typedef enum {
     MC_LIST_GRADS = 0,       /* grad_dtype                                                                         */
-    MC_LIST_CLIPPED = 1,     /* grad_dtype; what mc_grad_clip writes.  Not bound: the gradients themselves           */
+    MC_LIST_CLIPPED = 1,     /* grad_dtype; what mc_grad_clip writes.  Not bound, or
+                                bound to the same addresses: the gradients themselves                              */
     MC_LIST_PARAMS = 2,      /* fp32 weights                                                                       */
     MC_LIST_EXP_AVG = 3,     /* fp32 first moments                                                                 */
     MC_LIST_EXP_AVG_SQ = 4,  /* fp32 second moments                                                                */
@@ -56,8 +57,8 @@ typedef enum {
  *   model_dtype  mc_dtype of the model's copy of the weights: MC_DTYPE_BF16, MC_DTYPE_F16, or MC_DTYPE_NONE for no copy
  *   no_decay     host, n_tensors bytes, not 0 where mc_adamw's weight decay leaves a tensor out (biases, norms); may be NULL
  * Device memory: 16 bytes per 4096 elements of a tensor, 48 per tensor, about 20 KB besides.
- * Errors: MC_ERR_INVALID_ARG (null, n_tensors < 1, negative size, unknown type), MC_ERR_RANGE (a tensor of 2^43
- * elements or more, 2^31 blocks of 4096 elements in all), MC_ERR_ALLOC, MC_ERR_DEVICE.
+ * Errors: MC_ERR_INVALID_ARG (null, n_tensors < 1, negative size, unknown type), MC_ERR_RANGE (a tensor of 2^39
+ * elements or more, more than 2^27 blocks of 4096 elements in all), MC_ERR_ALLOC, MC_ERR_DEVICE.
  */
 int mc_step_create(mc_step **out, const int64_t *numel, int32_t n_tensors, int32_t grad_dtype, int32_t model_dtype,
                    const uint8_t *no_decay);

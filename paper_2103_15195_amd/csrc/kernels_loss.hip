@@ -633,7 +633,7 @@ template <class T>
 static uint32_t reach(const LossArgs &a, uint32_t line)
 {
     const uintptr_t at = (uintptr_t)a.logits, step = (uintptr_t)a.stride * sizeof(T);
-    const uintptr_t shift = step % line == 0 ? at % line : line - sizeof(T);
+    const uintptr_t shift = step % line == 0 || a.rows == 1u ? at % line : line - sizeof(T);
     return (uint32_t)((shift / sizeof(T) + a.vocab) / Raw<T>::N);
 }
 // At most kTermRows rows; whether their terms are added up.

@@ -97,9 +97,9 @@ int mc_step_create(mc_step **out, const int64_t *numel, int32_t n_tensors, int32
     uint64_t pieces = 0;
     for (int32_t t = 0; t < n_tensors; ++t) {
         if (numel[t] < 0) return MC_ERR_INVALID_ARG;
-        if (numel[t] >= (int64_t(1) << 43)) return MC_ERR_RANGE;
+        if (numel[t] >= (int64_t(1) << 39)) return MC_ERR_RANGE;
         pieces += numel[t] ? ((uint64_t)numel[t] + kMostShift + kPiece - 1) / kPiece : 0;
-        if (pieces >= (uint64_t(1) << 31)) return MC_ERR_RANGE;
+        if (pieces > (uint64_t(1) << 27)) return MC_ERR_RANGE;
     }
     mc_step *h = new (std::nothrow) mc_step();
     if (!h) return MC_ERR_ALLOC;

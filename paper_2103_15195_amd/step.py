@@ -128,6 +128,7 @@ class Step:
         B._check(lib().mc_step_create(C.byref(self._h), nm, n, self.dtypes["grads"], self.dtypes["model"], nd), "mc_step_create")
         self._at = self._h.value
         self._fast = lib().fast_step
+        self._device = torch.device("cuda", torch.cuda.current_device())
 
     def close(self) -> None:
         if getattr(self, "_h", None):
@@ -154,8 +155,8 @@ class Step:
             if len(tensors) != len(self.numel):
                 raise ValueError(f"{name}: {len(self.numel)} tensors, not {len(tensors)}")
             for i, (t, n) in enumerate(zip(tensors, self.numel)):
-                if t.numel() != n or not t.is_contiguous() or not t.is_cuda or DTYPE_IDS.get(t.dtype) != self.dtypes[name]:
-                    raise ValueError(f"{name}[{i}]: {n} contiguous elements on the device of the list's type, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+                if t.numel() != n or not t.is_contiguous() or t.device != self._device or DTYPE_IDS.get(t.dtype) != self.dtypes[name]:
+                    raise ValueError(f"{name}[{i}]: {n} contiguous elements of the list's type on {self._device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
         for name, tensors in lists.items():
             tensors = list(tensors)
             B._check(lib().mc_step_bind(self._h, LISTS[name], B.ptr_array(tensors), B._stream_handle(stream)), "mc_step_bind")
