@@ -138,24 +138,48 @@ __device__ __forceinline__ Term left_term(const Term *from)
     __builtin_memcpy(&t, x, sizeof t);
     return t;
 }
-// by all of a block's threads, behind their rows: the last block's first wavefront adds up the terms of all
-constexpr uint32_t kFewBlocks = 256;
+// By all of a block's threads, behind their rows: the last block adds up the terms of all.  In launches of at most so many threads over at most so many
+// rows.  (So and by a kernel behind, us: 600 x 8000 bf16 8.5 and 11.8, 4096 x 1000 10.2 and 11.8, 512 x 32000 14.1 and 14.6, 2048 x 8000 15.1 and 15.2; beyond the
+// lines 1024 x 32000 25.9 and 23.9, 8192 x 1000 15.2 and 12.4, 16384 x 100 17.1 and 11.7.)
+constexpr uint64_t kFewThreads = 1u << 19;
+constexpr uint32_t kFewRows = 4096;
+static bool sums_here(const LossArgs &a, uint32_t blocks, uint32_t threads) { return (uint64_t)blocks * threads <= kFewThreads && a.rows <= kFewRows && !a.more; }
+template <int THREADS>
 __device__ __forceinline__ void sum_here(const LossArgs &a)
 {
+    constexpr int WAVES = THREADS / 64;
+    __shared__ double lds[WAVES][kLossSums];
+    __shared__ uint32_t last;
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
     __builtin_amdgcn_s_waitcnt(0);               // each wavefront for the term that it has left: the barrier does not wait for stores
     __syncthreads();
-    if (threadIdx.x >= 64u || !arrives_last(a.counts)) return;
+    if (threadIdx.x < 64u) {
+        const bool mine = arrives_last(a.counts);
+        if (threadIdx.x == 0) last = mine;
+    }
+    __syncthreads();
+    if (!last) return;
+    const uint32_t lane = threadIdx.x & 63u;
     Sums s;
-    for (uint32_t i = threadIdx.x; i < a.rows; i += 64u * 4u) {
+    for (uint32_t i = threadIdx.x; i < a.rows; i += THREADS * 4u) {
         Term t[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) if (i + 64u * k < a.rows) t[k] = left_term(a.terms + i + 64u * k); else t[k].kind = TERM_NONE;
+        for (int k = 0; k < 4; ++k) if (i + (uint32_t)(THREADS * k) < a.rows) t[k] = left_term(a.terms + i + (uint32_t)(THREADS * k)); else t[k].kind = TERM_NONE;
 #pragma unroll
         for (int k = 0; k < 4; ++k) s.add(t[k]);
     }
     const double mine = s.join();
-    put_sums(a, __shfl(mine, (int)sum_of_lane(), 64), s.taken, s.left_out);      // (sum_of_lane is its own inverse on 0..3)
+    double *w = lds[threadIdx.x >> 6];
+    if (lane < 4u) w[sum_of_lane()] = mine;
+    if (lane == 0) { w[4] = (double)s.taken; w[5] = (double)s.left_out; }
+    __syncthreads();
+    if (threadIdx.x >= 64u) return;
+    double sum = 0.0;
+    if (lane < (uint32_t)kLossSums)
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) sum += lds[k][lane];
+    const uint32_t taken = (uint32_t)__shfl(sum, 4, 64), left_out = (uint32_t)__shfl(sum, 5, 64);
+    put_sums(a, sum, taken, left_out);
 }
 // A block for every kTermBlock rows, all of whose terms it asks for at once.  The sums of the rows of earlier launches stand behind the parts.
 constexpr int kTermThreads = 512;
@@ -401,7 +425,7 @@ __global__ __launch_bounds__(SHARE < kBlock ? kBlock : SHARE, NV <= 4 ? 8 : 4) v
         if (lane == span.template owner<SHARE>((uint32_t)row.label)) dx[row.label] = (T)(part * row_exp<T>(a, xa, wbase) + slope);
     };
     if (r < a.rows) body();
-    if (HERE) sum_here(a);
+    if (HERE) sum_here<THREADS>(a);
 }
 
 // ---- longer rows --------------------------------------------------------------------------------------------------------------
@@ -512,7 +536,7 @@ __global__ __launch_bounds__(1024, LOSS ? 4 : 8) void loss_long_k(LossArgs a)
         if (lane == span.template owner<SHARE>((uint32_t)row.label)) dx[row.label] = (T)(part * row_exp<T>(a, xa, top) + slope);
     };
     body();
-    if (HERE) sum_here(a);
+    if (HERE) sum_here<1024>(a);
 }
 
 // ---- few rows -----------------------------------------------------------------------------------------------------------------
@@ -615,7 +639,7 @@ __global__ __launch_bounds__(kBlock) void loss_join_k(LossArgs a, uint32_t parts
         if (part == (in_vector ? i / kPartVecs : 0u) && lane == span.template owner<kBlock>((uint32_t)row.label)) dx[row.label] = (T)(scale * row_exp<T>(a, xa, top) + slope);
     };
     body();
-    if (LOSS) sum_here(a);
+    if (LOSS) sum_here<kBlock>(a);
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------------
@@ -624,7 +648,7 @@ static bool held(const LaunchCtx &lc, const LossArgs &a)
 {
     constexpr uint32_t THREADS = SHARE < kBlock ? kBlock : SHARE, each = THREADS / SHARE;
     const uint32_t blocks = (a.rows + each - 1) / each;
-    const bool here = LOSS && blocks <= kFewBlocks && !a.more;
+    const bool here = LOSS && sums_here(a, blocks, THREADS);
     launch(here ? loss_held_k<T, SHARE, NV, KEEP, LOSS, LOSS> : loss_held_k<T, SHARE, NV, KEEP, LOSS, false>, dim3(blocks), dim3(THREADS), lc.stream, a);
     return here;
 }
@@ -672,7 +696,7 @@ static bool loss_of(const LaunchCtx &lc, LossArgs a)
     // (log-probabilities alone are read once in any case: 2048 rows of 128259 62 us held, 56 not)
     if (LOSS && vecs <= 1024 * 8) return held<T, 1024, 8, false, LOSS>(lc, a);
     if (LOSS && vecs <= 1024 * 16) return held<T, 1024, 16, false, LOSS>(lc, a);
-    const bool here = LOSS && a.rows <= kFewBlocks && !a.more;
+    const bool here = LOSS && sums_here(a, a.rows, 1024u);
     launch(here ? loss_long_k<T, LOSS, LOSS> : loss_long_k<T, LOSS, false>, dim3(a.rows), dim3(1024), lc.stream, a);
     return here;
 }
