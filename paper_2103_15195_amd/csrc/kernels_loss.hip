@@ -26,13 +26,6 @@ __device__ __forceinline__ double log_wide(float x)
     return (double)e * 0.693147180559945309 + (double)logf(f);
 }
 
-__device__ __forceinline__ float wave_sum_f(float x)
-{
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, 64);
-    return x;
-}
-
 // What a row is besides its logits, all asked for at once.  Where a wavefront has one row, this comes through the scalar cache and stays in scalar
 // registers.
 struct Row {
@@ -81,8 +74,8 @@ __device__ __forceinline__ RowTerms row_terms(const LossArgs &a, const Row &row,
 }
 
 // ---- sums over rows ---------------------------------------------------------------------------------------------------
-// The rows' kernels leave a Term for every row.  In launches of few blocks the last one adds them up; in larger ones, where that
-// block would find thousands of them and every block would wait for its terms to be written through, a kernel behind them does.
+// The rows' kernels leave a Term for every row.  In launches of few threads the last block adds them up; in larger ones, where that
+// block would find thousands of them and every block would wait for its terms to be written through, a kernel behind them does (4.6 us of its own).
 struct Sums {
     double at[4] = {};           // weight times policy term, KL term, whether the clamp decides, 1
     uint32_t taken = 0, left_out = 0;
@@ -125,8 +118,8 @@ __device__ __forceinline__ void put_sums(const LossArgs &a, double sum, uint32_t
 // a term past the caches, to a block that may sit on another die, and there
 __device__ __forceinline__ void leave_term(Term *to, const Term &t)
 {
-    const uint64_t *from = reinterpret_cast<const uint64_t *>(&t);
-    uint64_t *p = reinterpret_cast<uint64_t *>(to);
+    uint64_t from[2], *p = reinterpret_cast<uint64_t *>(to);
+    __builtin_memcpy(from, &t, sizeof t);
     __hip_atomic_store(p, from[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __hip_atomic_store(p + 1, from[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -662,8 +655,8 @@ static uint32_t reach(const LossArgs &a, uint32_t line)
 }
 // At most kTermRows rows; whether their terms are added up.
 // Threads to a row: few enough for several rows to a wavefront where rows are short (32768 x 200 / 500 / 1000 bf16 with 16, 32 and 64 threads to a row: 12.9 /
-// 21.5 / 27.9, 15.2 / 19.8 / 31.1 and 19.7 / 22.2 / 27.7 us), else as few as hold it in the registers that let 32 wavefronts share a compute unit (64), up to 65536 elements of 16 bits; of longer
-// rows twice that.  Rates of the policy loss in bf16 (TB/s): 4096 x 32064 5.5, 32003 (rows begin anywhere) 5.5, both with one row in eight masked; with 40 %
+// 21.5 / 27.9, 15.2 / 19.8 / 31.1 and 19.7 / 22.2 / 27.7 us), else as few as hold it in the registers that let 32 wavefronts share a compute unit (64 a
+// thread, up to 65536 elements of 16 bits); for longer rows twice those.  Rates of the policy loss in bf16 (TB/s): 4096 x 32064 5.5, 32003 (rows begin anywhere) 5.5, both with one row in eight masked; with 40 %
 // masked 4096 x 32064 5.3, 8192 x 8192 4.9, 16384 x 4096 5.1, 32768 x 1000 3.9, 65536 x 100 1.4, 2048 x 65536 5.1, 2048 x 128259 5.3, 1024 x 200001 5.0.
 template <class T, bool LOSS>
 static bool loss_of(const LaunchCtx &lc, LossArgs a)
@@ -694,8 +687,10 @@ static bool loss_of(const LaunchCtx &lc, LossArgs a)
     if (vecs <= 1024 * 2) return held<T, 1024, 2, true, LOSS>(lc, a);
     if (vecs <= 1024 * 4) return held<T, 1024, 4, true, LOSS>(lc, a);
     // (log-probabilities alone are read once in any case: 2048 rows of 128259 62 us held, 56 not)
-    if (LOSS && vecs <= 1024 * 8) return held<T, 1024, 8, false, LOSS>(lc, a);
-    if (LOSS && vecs <= 1024 * 16) return held<T, 1024, 16, false, LOSS>(lc, a);
+    if constexpr (LOSS) {
+        if (vecs <= 1024 * 8) return held<T, 1024, 8, false, LOSS>(lc, a);
+        if (vecs <= 1024 * 16) return held<T, 1024, 16, false, LOSS>(lc, a);
+    }
     const bool here = LOSS && sums_here(a, a.rows, 1024u);
     launch(here ? loss_long_k<T, LOSS, LOSS> : loss_long_k<T, LOSS, false>, dim3(a.rows), dim3(1024), lc.stream, a);
     return here;

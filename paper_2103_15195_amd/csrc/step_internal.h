@@ -121,9 +121,9 @@ MC_VEC(_Float16, 4, 2);
 MC_VEC(_Float16, 8, 2);
 #undef MC_VEC
 
-// N consecutive elements from p + i, of those from `lo` to `hi` (the others: `fill`).  STREAM: not to be kept in the caches.
+// N consecutive elements from p + i, of those from `lo` to `hi` (the others: 0).  STREAM: not to be kept in the caches.
 template <int N, class T, bool STREAM = true>
-__device__ __forceinline__ void load_some(global_ptr<const T> p, int32_t i, int32_t lo, int32_t hi, float (&v)[N], float fill = 0.0f)
+__device__ __forceinline__ void load_some(global_ptr<const T> p, int32_t i, int32_t lo, int32_t hi, float (&v)[N])
 {
     typedef typename VecOf<T, N>::type vec;
     if (i >= lo && i + N <= hi) {
@@ -133,7 +133,7 @@ __device__ __forceinline__ void load_some(global_ptr<const T> p, int32_t i, int3
         for (int e = 0; e < N; ++e) v[e] = (float)x[e];
     } else {
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = i + e >= lo && i + e < hi ? (float)p[i + e] : fill;
+        for (int e = 0; e < N; ++e) v[e] = i + e >= lo && i + e < hi ? (float)p[i + e] : 0.0f;
     }
 }
 template <int N, class T>
