@@ -325,11 +325,12 @@ struct RowSpan {
 
 // SHARE threads to a row, each with up to NV 16-byte vectors of it, which are read once, and perhaps an element of its edge.
 // KEEP: the exponentials stay in registers between the sum and the gradient, else the logits do.  HERE: the last block adds up
-// the rows' terms.
+// the rows' terms.  Rows of one wavefront or less share a block of kBlock threads; those of more have one to themselves, since they meet at a barrier.
+template <int SHARE> constexpr int held_threads() { return SHARE <= 64 ? kBlock : SHARE; }
 template <class T, int SHARE, int NV, bool KEEP, bool LOSS, bool HERE>
-__global__ __launch_bounds__(SHARE < kBlock ? kBlock : SHARE, NV <= 4 ? 8 : 4) void loss_held_k(LossArgs a)
+__global__ __launch_bounds__(held_threads<SHARE>(), NV <= 4 || SHARE <= 512 ? 8 : 4) void loss_held_k(LossArgs a)
 {
-    constexpr int THREADS = SHARE < kBlock ? kBlock : SHARE, N = Raw<T>::N, WAVES = SHARE / 64;
+    constexpr int THREADS = held_threads<SHARE>(), N = Raw<T>::N, WAVES = SHARE / 64;
     constexpr bool ONE = SHARE >= 64;
     typedef typename VecOf<T, N>::type out_vec;
     __shared__ float at[2 * WAVES + 1];
@@ -639,7 +640,7 @@ __global__ __launch_bounds__(kBlock) void loss_join_k(LossArgs a, uint32_t parts
 template <class T, int SHARE, int NV, bool KEEP, bool LOSS>
 static bool held(const LaunchCtx &lc, const LossArgs &a)
 {
-    constexpr uint32_t THREADS = SHARE < kBlock ? kBlock : SHARE, each = THREADS / SHARE;
+    constexpr uint32_t THREADS = held_threads<SHARE>(), each = THREADS / SHARE;
     const uint32_t blocks = (a.rows + each - 1) / each;
     const bool here = LOSS && sums_here(a, blocks, THREADS);
     launch(here ? loss_held_k<T, SHARE, NV, KEEP, LOSS, LOSS> : loss_held_k<T, SHARE, NV, KEEP, LOSS, false>, dim3(blocks), dim3(THREADS), lc.stream, a);
@@ -654,10 +655,13 @@ static uint32_t reach(const LossArgs &a, uint32_t line)
     return (uint32_t)((shift / sizeof(T) + a.vocab) / Raw<T>::N);
 }
 // At most kTermRows rows; whether their terms are added up.
-// Threads to a row: few enough for several rows to a wavefront where rows are short (32768 x 200 / 500 / 1000 bf16 with 16, 32 and 64 threads to a row: 12.9 /
-// 21.5 / 27.9, 15.2 / 19.8 / 31.1 and 19.7 / 22.2 / 27.7 us), else as few as hold it in the registers that let 32 wavefronts share a compute unit (64 a
-// thread, up to 65536 elements of 16 bits); for longer rows twice those.  Rates of the policy loss in bf16 (TB/s): 4096 x 32064 5.5, 32003 (rows begin anywhere) 5.5, both with one row in eight masked; with 40 %
-// masked 4096 x 32064 5.3, 8192 x 8192 4.9, 16384 x 4096 5.1, 32768 x 1000 3.9, 65536 x 100 1.4, 2048 x 65536 5.1, 2048 x 128259 5.3, 1024 x 200001 5.0.
+// Threads to a row, and vectors that each holds: several rows to a wavefront where rows are short (32768 x 200 / 500 / 1000 bf16 with 16, 32 and 64
+// threads to a row: 12.9 / 21.5 / 27.9, 15.2 / 19.8 / 31.1 and 19.7 / 22.2 / 27.7 us), then so that few of the threads have less to hold than others, in at most the 64 registers
+// that let 32 wavefronts share a compute unit (up to 65536 elements of 16 bits; for longer rows twice those).  80 M logits in rows of 10000 / 12000 / 14000 / 16000 bf16 by
+// 1024 threads of two vectors 65 / 57 / 53 / 52 us, by 512 of three or four 51 / 51 / 53 / 53; 2000 / 8000 by 64 / 256 of four 56 / 52, by 128 / 512 of two 55 / 51.
+// Without a gradient to write fewer threads with more to read are ahead: rows of 10000 / 16000 by 1024 of two 39 / 28, by 256 of eight 25 / 21.
+// Rates of the policy loss in bf16 (TB/s): 4096 x 32064 5.5, 32003 (rows begin anywhere) 5.5, both with one row in eight masked; with 40 %
+// masked 4096 x 32064 5.3, 8192 x 8192 5.0, 16384 x 4096 5.1, 32768 x 1000 3.9, 65536 x 100 1.4, 2048 x 65536 5.1, 2048 x 128259 5.3, 1024 x 200001 5.0.
 template <class T, bool LOSS>
 static bool loss_of(const LaunchCtx &lc, LossArgs a)
 {
@@ -665,7 +669,7 @@ static bool loss_of(const LaunchCtx &lc, LossArgs a)
     // (a row that would need twice the registers for it is not moved to a line)
     const uint32_t close = reach<T>(a, 16u);
     uint32_t vecs = reach<T>(a, kLine);
-    for (uint32_t room : {16u, 32u, 64u, 128u, 256u, 512u, 1024u, 2048u, 4096u, 8192u, 16384u}) if (close <= room && room < vecs) { a.line = 16u; vecs = close; }
+    for (uint32_t room : {16u, 32u, 64u, 128u, 256u, 384u, 512u, 768u, 1024u, 1536u, 2048u, 3072u, 4096u, 8192u, 16384u}) if (close <= room && room < vecs) { a.line = 16u; vecs = close; }
     // Few long rows are shared by blocks.  (Policy loss so and with a block to each, us: rows of 128256 bf16, 1 / 64 / 128 / 200 of them 13.6 / 14.0 / 19.0 / 27.5
     // and 18.2 / 21.0 / 21.7 / 23.7; of 262144 fp32 13.6 / 30.8 / 56.9 / 88.3 and 42.9 / 51.6 / 71.0 / 97.0; of 70000 bf16, 64 / 128 / 200 13.1 / 15.1 / 17.6 and
     // 17.1 / 17.6 / 18.3.  Below 8192 vectors the second launch costs more than it gains: 1 / 64 of 64000 bf16 13.5 / 13.3 and 11.8 / 14.0, their
@@ -681,15 +685,27 @@ static bool loss_of(const LaunchCtx &lc, LossArgs a)
     if (vecs <= 16 * 2) return held<T, 16, 2, true, LOSS>(lc, a);
     if (vecs <= 32 * 2) return held<T, 32, 2, true, LOSS>(lc, a);
     if (vecs <= 64 * 2) return held<T, 64, 2, true, LOSS>(lc, a);
-    if (vecs <= 64 * 4) return held<T, 64, 4, true, LOSS>(lc, a);
-    if (vecs <= 256 * 2) return held<T, 256, 2, true, LOSS>(lc, a);
-    if (vecs <= 256 * 4) return held<T, 256, 4, true, LOSS>(lc, a);
-    if (vecs <= 1024 * 2) return held<T, 1024, 2, true, LOSS>(lc, a);
-    if (vecs <= 1024 * 4) return held<T, 1024, 4, true, LOSS>(lc, a);
-    // (log-probabilities alone are read once in any case: 2048 rows of 128259 62 us held, 56 not)
     if constexpr (LOSS) {
+        if (vecs <= 128 * 2) return held<T, 128, 2, true, LOSS>(lc, a);
+        if (vecs <= 128 * 3) return held<T, 128, 3, true, LOSS>(lc, a);
+        if (vecs <= 256 * 2) return held<T, 256, 2, true, LOSS>(lc, a);
+        if (vecs <= 256 * 3) return held<T, 256, 3, true, LOSS>(lc, a);
+        if (vecs <= 512 * 2) return held<T, 512, 2, true, LOSS>(lc, a);
+        if (vecs <= 512 * 3) return held<T, 512, 3, true, LOSS>(lc, a);
+        if (vecs <= 1024 * 2) return held<T, 1024, 2, true, LOSS>(lc, a);
+        if (vecs <= 1024 * 3) return held<T, 1024, 3, true, LOSS>(lc, a);
+        if (vecs <= 1024 * 4) return held<T, 1024, 4, true, LOSS>(lc, a);
         if (vecs <= 1024 * 8) return held<T, 1024, 8, false, LOSS>(lc, a);
         if (vecs <= 1024 * 16) return held<T, 1024, 16, false, LOSS>(lc, a);
+    } else {
+        // (log-probabilities alone are read once in any case: 2048 rows of 128259 62 us held, 56 not)
+        if (vecs <= 64 * 4) return held<T, 64, 4, true, LOSS>(lc, a);
+        if (vecs <= 128 * 3) return held<T, 128, 3, true, LOSS>(lc, a);
+        if (vecs <= 128 * 4) return held<T, 128, 4, true, LOSS>(lc, a);
+        if (vecs <= 256 * 3) return held<T, 256, 3, true, LOSS>(lc, a);
+        if (vecs <= 256 * 4) return held<T, 256, 4, true, LOSS>(lc, a);
+        if (vecs <= 256 * 8) return held<T, 256, 8, false, LOSS>(lc, a);
+        if (vecs <= 512 * 8) return held<T, 512, 8, false, LOSS>(lc, a);
     }
     const bool here = LOSS && sums_here(a, a.rows, 1024u);
     launch(here ? loss_long_k<T, LOSS, LOSS> : loss_long_k<T, LOSS, false>, dim3(a.rows), dim3(1024), lc.stream, a);
