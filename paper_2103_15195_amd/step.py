@@ -144,21 +144,20 @@ class Step:
             pass
 
     def bind(self, stream=None, **lists) -> None:
-        """Hands over lists of tensors, one tensor for each of the model: grads, clipped, params, exp_avg, exp_avg_sq, model.
+        """Hands over lists of tensors (any iterables), one tensor for each of the model: grads, clipped, params, exp_avg, exp_avg_sq, model.
         A list holds until it is handed over again; its tensors are kept alive until then."""
+        lists = {name: list(tensors) for name, tensors in lists.items()}         # gone through once: it may be a generator
         for name, tensors in lists.items():
             if name not in LISTS:
                 raise ValueError(f"{name}: one of {', '.join(LISTS)}")
             if name == "model" and self.dtypes["model"] == MC_DTYPE_NONE:
                 raise ValueError("model: the handle was made without a model_dtype")
-            tensors = list(tensors)
             if len(tensors) != len(self.numel):
                 raise ValueError(f"{name}: {len(self.numel)} tensors, not {len(tensors)}")
             for i, (t, n) in enumerate(zip(tensors, self.numel)):
                 if t.numel() != n or not t.is_contiguous() or t.device != self._device or DTYPE_IDS.get(t.dtype) != self.dtypes[name]:
                     raise ValueError(f"{name}[{i}]: {n} contiguous elements of the list's type on {self._device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
         for name, tensors in lists.items():
-            tensors = list(tensors)
             B._check(lib().mc_step_bind(self._h, LISTS[name], B.ptr_array(tensors), B._stream_handle(stream)), "mc_step_bind")
             self._kept[name] = tensors
 
