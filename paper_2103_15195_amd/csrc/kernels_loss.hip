@@ -53,6 +53,14 @@ __device__ __forceinline__ Row row_of(const LossArgs &a, uint32_t r)
     return row;
 }
 
+// exp(d) - d - 1, with em = exp(d) - 1: near 0, where the difference would be d^2 / 2 of two numbers of size d, by its series (of which
+// the first term left out is less than a twentieth of a unit in the last place).
+__device__ __forceinline__ float kl_term(float d, float em)
+{
+    float p = 1.0f / 362880.0f;
+    for (const float c : {1.0f / 40320.0f, 1.0f / 5040.0f, 1.0f / 720.0f, 1.0f / 120.0f, 1.0f / 24.0f, 1.0f / 6.0f, 0.5f}) p = __builtin_fmaf(p, d, c);
+    return fabsf(d) < 0.5f ? d * d * p : em - d;
+}
 // What a row adds to the sums, and the slope of its loss by its log-probability l.
 struct RowTerms { float policy, kl, slope; bool cut; };
 __device__ __forceinline__ RowTerms row_terms(const LossArgs &a, const Row &row, double l)
@@ -66,9 +74,9 @@ __device__ __forceinline__ RowTerms row_terms(const LossArgs &a, const Row &row,
     t.cut = !is_free;
     t.kl = 0.0f;
     if (a.ref_logp) {
-        const float d = (float)((double)row.ref - l), ed = expf(d);
-        t.kl = ed - d - 1.0f;
-        t.slope += a.kl_coef * (1.0f - ed);
+        const float d = (float)((double)row.ref - l), em = expm1f(d);
+        t.kl = kl_term(d, em);
+        t.slope -= a.kl_coef * em;
     }
     return t;
 }
