@@ -7,13 +7,13 @@ constexpr float kNone = -__builtin_inff();
 
 // exp((x - top) / temperature) for logits of type T.  The difference comes first, so that a row of nothing but the type's lowest
 // value is as good as any other.  With logits of 32 bits the factor has a second part: rounded to 24 bits it moves
-// exp(-10) by 4e-7 (what is infinite already stays away from that part: times 0 or a negative number it would be NaN).
+// exp(-10) by 4e-7 (the product with it is kept finite: an infinite one of the other sign would make NaN of the sum).
 template <class T>
 __device__ __forceinline__ float row_exp(const LossArgs &a, float x, float top)
 {
     const float d = x - top;
     if constexpr (sizeof(T) < 4) return __builtin_amdgcn_exp2f(d * a.to_base2);
-    return __builtin_amdgcn_exp2f(__builtin_fmaf(d, a.to_base2, fmaxf(d, -1e30f) * a.to_base2_rest));
+    return __builtin_amdgcn_exp2f(__builtin_fmaf(d, a.to_base2, fmaxf(d, a.least) * a.to_base2_rest));
 }
 // where a maximum of minus infinity (nothing seen so far) stands for exponents: any finite number
 __device__ __forceinline__ float base_of(float top) { return top == kNone ? 0.0f : top; }

@@ -1,4 +1,5 @@
 // Host side of the C ABI declared in include/mergecomp_step.h: handles, argument checks and launches.
+#include <cfloat>
 #include <cmath>
 #include <new>
 #include <vector>
@@ -238,6 +239,9 @@ static int logits_args(const mc_loss *h, const mc_logits *x, LossArgs &a)
     a.to_base2 = (float)base2;
     if (!std::isfinite(a.to_base2)) return MC_ERR_INVALID_ARG;          // (a temperature below 4.3e-39)
     a.to_base2_rest = (float)(base2 - (double)a.to_base2);
+    // (The first part is at least 2^24 times the second: with a second part above 1 the exponential of a difference beyond this is 0 whatever is
+    // added, and with a smaller one nothing finite lies beyond it but the last thousandth of binary32's range.)
+    a.least = -(float)(0.999 * FLT_MAX / std::fmax(1.0, std::fabs((double)a.to_base2_rest)));
     a.inv_t = 1.0 / (double)x->temperature;
     a.partial = h->d_partial;
     a.terms = h->d_terms;

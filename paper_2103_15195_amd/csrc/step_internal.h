@@ -67,6 +67,7 @@ struct LossArgs {
     int64_t stride, dstride;
     uint32_t rows, vocab;
     float to_base2, to_base2_rest;           // log2(e) / temperature, in two parts
+    float least;                             // below 0: the largest number whose product with the second part is finite
     double inv_t;
     float lo, hi, kl_coef, gscale;           // gscale: grad_scale / temperature
     Term *terms;                             // kTermRows
