@@ -67,7 +67,8 @@ __device__ __forceinline__ RowTerms row_terms(const LossArgs &a, const Row &row,
 {
     RowTerms t;
     const float adv = row.adv, rho = expf((float)(l - (double)row.old));
-    const float free = -adv * rho, held = -adv * fminf(fmaxf(rho, a.lo), a.hi);
+    // (without an advantage 0 times the ratio, which may be beyond binary32)
+    const float free = adv == 0.0f && rho > a.hi ? 0.0f : -adv * rho, held = -adv * fminf(fmaxf(rho, a.lo), a.hi);
     const bool is_free = !(free < held);              // (NaN: the ratio's)
     t.policy = is_free ? free : held;
     t.slope = is_free ? free : 0.0f;
