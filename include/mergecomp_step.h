@@ -17,6 +17,7 @@
  *   - Arithmetic is binary32; sums over tensors and over rows are binary64.  Sums are taken in an order that depends on sizes, on where
  *     rows and tensors begin in a cache line, and on the device alone: the same call gives the same bits.  Values of 16
  *     bits are widened when they are read and rounded once, to nearest even, when they are written.
+ *   - What a call writes may not lie over anything else that it writes or reads, except where it is said below.
  *   - Tensors may start at any address that is a multiple of their element size; multiples of 16 bytes are fastest.
  */
 #ifndef MERGECOMP_STEP_H
@@ -122,8 +123,8 @@ typedef struct {
  * logp[r] = x_a - log(sum_j exp(x_j)), x the row's logits / temperature, a its label.
  * A row whose label lies outside [0, vocab) is not read; its logp is 0.
  *   logp   device, rows floats
- * Errors: MC_ERR_INVALID_ARG (null, negative sizes, vocab < 1, stride < vocab, unknown type, misaligned pointers, temperature),
- * MC_ERR_RANGE (vocab of 2^31 - 2^16 or more, rows of 2^31 or more).
+ * Errors: MC_ERR_INVALID_ARG (null, negative sizes, vocab < 1, stride < vocab, unknown type, misaligned pointers, temperature,
+ * logp over labels or logits), MC_ERR_RANGE (vocab of 2^31 - 2^16 or more, rows of 2^31 or more).
  */
 int mc_token_logp(mc_loss *h, const mc_logits *x, float *logp, void *stream);
 
@@ -147,11 +148,12 @@ typedef struct {
                                  that take part, rows with a weight but no valid label; then 0  */
     float *logp;              /* device, rows, 0 where a row takes no part; may be NULL           */
     void *dlogits;            /* device, the logits' type; may be NULL (no gradient) or the logits themselves, of the same stride, but may
-                                 not overlap them otherwise                                    */
+                                 not overlap them otherwise (columns or rows between theirs are no overlap)   */
     int64_t dlogits_stride;
 } mc_policy;
 /* Errors: as mc_token_logp, and MC_ERR_INVALID_ARG for null old_logp, advantages or sums, clip_low outside [0, 1], clip_high
- * or kl_coef negative, anything not finite. */
+ * or kl_coef negative, anything not finite, logp or dlogits over anything else, sums over either (or, with more than 2^17 rows, over
+ * what is read). */
 int mc_policy_loss(mc_loss *h, const mc_logits *x, const mc_policy *p, void *stream);
 
 #ifdef __cplusplus

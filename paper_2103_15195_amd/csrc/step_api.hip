@@ -70,6 +70,41 @@ int grab_counts(uint32_t **p)
     return hipMemset(*p, 0, kArriveBytes) == hipSuccess && hipDeviceSynchronize() == hipSuccess ? MC_OK : MC_ERR_DEVICE;
 }
 
+// ---- whether two things in memory share a byte
+struct Span {
+    uintptr_t at;
+    uint64_t bytes;
+};
+Span span(const void *p, uint64_t bytes) { return {reinterpret_cast<uintptr_t>(p), p ? bytes : 0u}; }
+bool meet(Span a, Span b) { return a.bytes && b.bytes && a.at < b.at + b.bytes && b.at < a.at + a.bytes; }
+// The rows of a matrix: `rows` of them, `bytes` each (not 0), `step` from one to the next.
+struct RowsAt {
+    uintptr_t at;
+    uint64_t rows, bytes, step;
+    // (a step that no address space holds stands for all longer ones, so that sums of an address and a step stay below 2^64)
+    RowsAt(const void *p, int64_t n, int64_t vocab, int64_t stride, uintptr_t size)
+        : at(reinterpret_cast<uintptr_t>(p)), rows(p ? (uint64_t)n : 0u), bytes((uint64_t)vocab * size), step((uint64_t)(stride < (int64_t(1) << 58) ? stride : int64_t(1) << 58) * size) {}
+    Span all() const { return {at, rows ? (rows > (uint64_t(1) << 62) / step ? uint64_t(1) << 62 : (rows - 1u) * step) + bytes : 0u}; }
+};
+bool meet(Span a, const RowsAt &m)
+{
+    if (!meet(a, m.all())) return false;
+    const uint64_t k = a.at > m.at ? (a.at - m.at) / m.step : 0u;                 // the last row that begins at a or before it, or the first
+    return meet(a, Span{m.at + k * m.step, m.bytes}) || (k + 1u < m.rows && meet(a, Span{m.at + (k + 1u) * m.step, m.bytes}));
+}
+// (of as many rows)
+bool meet(const RowsAt &a, const RowsAt &b)
+{
+    if (!meet(a.all(), b.all())) return false;
+    if (a.step != b.step) {            // (and in one another's reach: no layout that a program would choose)
+        for (uint64_t k = 0; k < a.rows; ++k) if (meet(Span{a.at + k * a.step, a.bytes}, b)) return true;
+        return false;
+    }
+    // rows of one step lie on each other where the distance of the two is closer to a multiple of it than a row is long
+    const uint64_t distance = a.at > b.at ? a.at - b.at : b.at - a.at, k = distance / a.step, behind = distance % a.step;
+    return (k < a.rows && behind < a.bytes) || (k + 1u < a.rows && a.step - behind < a.bytes);
+}
+
 }  // namespace
 
 extern "C" {
@@ -256,9 +291,25 @@ int mc_token_logp(mc_loss *h, const mc_logits *x, float *logp, void *stream)
     const int rc = logits_args(h, x, a);
     if (rc != MC_OK) return rc;
     if ((a.rows && !logp) || off(logp, 4)) return MC_ERR_INVALID_ARG;
+    const Span to = span(logp, 4u * (uint64_t)a.rows);
+    if (meet(to, span(x->labels, 8u * (uint64_t)a.rows)) || meet(to, RowsAt(x->logits, x->rows, x->vocab, x->stride, size_of(x->dtype)))) return MC_ERR_INVALID_ARG;
     a.logp = logp;
     launch_token_logp(on(stream), x->dtype, a);
     return launched();
+}
+
+// Whether anything that a call writes lies over something else of it.  Wavefronts and blocks that share a row read and write what the row has in no order, so
+// that a log-probability in the place of an old one, say, could be taken for it.  The sums come behind the rows whose terms they hold, so they may lie over what
+// is read, unless there are more rows to come.
+static bool overlaps(const mc_logits *x, const mc_policy *p)
+{
+    const uint64_t n = (uint64_t)x->rows;
+    const Span logp = span(p->logp, 4u * n), sums = span(p->sums, 32u);
+    const RowsAt logits(x->logits, x->rows, x->vocab, x->stride, size_of(x->dtype)), slopes(p->dlogits, x->rows, x->vocab, p->dlogits_stride, size_of(x->dtype));
+    for (const Span s : {span(x->labels, 8u * n), span(p->old_logp, 4u * n), span(p->advantages, 4u * n), span(p->weights, 4u * n), span(p->ref_logp, 4u * n)})
+        if (meet(logp, s) || meet(s, slopes) || (n > kTermRows && meet(sums, s))) return true;
+    if (meet(logp, sums) || meet(logp, logits) || meet(logp, slopes) || meet(sums, slopes) || (n > kTermRows && meet(sums, logits))) return true;
+    return p->dlogits != x->logits && meet(slopes, logits);
 }
 
 int mc_policy_loss(mc_loss *h, const mc_logits *x, const mc_policy *p, void *stream)
@@ -271,6 +322,7 @@ int mc_policy_loss(mc_loss *h, const mc_logits *x, const mc_policy *p, void *str
                           (const void *)p->logp}) if (off(q, 4)) return MC_ERR_INVALID_ARG;
     if (p->dlogits && (off(p->dlogits, size_of(x->dtype)) || p->dlogits_stride < x->vocab)) return MC_ERR_INVALID_ARG;
     if (p->dlogits == x->logits && p->dlogits && p->dlogits_stride != x->stride) return MC_ERR_INVALID_ARG;
+    if (overlaps(x, p)) return MC_ERR_INVALID_ARG;
     if (!(p->clip_low >= 0.0f && p->clip_low <= 1.0f && p->clip_high >= 0.0f && p->kl_coef >= 0.0f)) return MC_ERR_INVALID_ARG;
     if (!std::isfinite(p->clip_high) || !std::isfinite(p->kl_coef) || !std::isfinite(p->grad_scale)) return MC_ERR_INVALID_ARG;
     a.old_logp = p->old_logp; a.advantages = p->advantages; a.weights = p->weights; a.ref_logp = p->ref_logp;
