@@ -222,12 +222,14 @@ typedef int (*adamw_fn)(void *, const Adamw *, const void *, void *);
 typedef int (*token_logp_fn)(void *, const Logits *, void *, void *);
 typedef int (*policy_loss_fn)(void *, const Logits *, const Policy *, void *);
 
-PyObject *g_dtype, *g_is_cuda, *g_shape, *g_stride;      // names
+PyObject *g_dtype, *g_is_cuda, *g_get_device, *g_shape, *g_stride;      // names
 
-// The entry points, and torch's types: of values by their numbers there, and of labels.
+// The entry points, torch's types (of values by their numbers there, and of labels), and the device that all tensors and the current stream
+// have to be on, by its index; -1: tensors on any.
 struct StepCalls {
     PyObject_HEAD
     PyObject *kinds[3], *int64;
+    long device;
     token_logp_fn token_logp;
     policy_loss_fn policy_loss;
     grad_norm_fn grad_norm, grad_clip;
@@ -238,6 +240,28 @@ bool is_true(PyObject *o, PyObject *name)
     PyObject *x = PyObject_GetAttr(o, name);
     Py_XDECREF(x);                    // (a bool: the interpreter's own)
     return x == Py_True;
+}
+bool is_here(const StepCalls *c, PyObject *o)
+{
+    if (c->device < 0) return is_true(o, g_is_cuda);
+    PyObject *d = PyObject_CallMethodNoArgs(o, g_get_device);
+    const long at = d ? PyLong_AsLong(d) : -1;        // (host memory: -1)
+    Py_XDECREF(d);
+    return at == c->device;
+}
+// the current stream, if the device that it is on is the one
+bool stream_here(const StepCalls *c, PyObject *callable, void **p)
+{
+    if (c->device < 0 || Py_TYPE(callable) != &RawStreamType) return stream_of(callable, p);
+    const RawStream *r = reinterpret_cast<const RawStream *>(callable);
+    PyObject *d = PyObject_CallNoArgs(r->device);
+    if (!d) return false;
+    PyObject *s = PyLong_AsLong(d) == c->device ? PyObject_CallOneArg(r->get, d) : nullptr;
+    Py_DECREF(d);
+    if (!s) return false;
+    const bool ok = address(s, p);
+    Py_DECREF(s);
+    return ok;
 }
 // whether the tensor's type is `kind`
 bool of_kind(PyObject *o, PyObject *kind)
@@ -261,13 +285,13 @@ bool layout(PyObject *o, int n, int64_t *size, int64_t *step)
     return ok;
 }
 // a device tensor of one dimension, `count` contiguous elements of a type; None only where allowed
-bool vector(PyObject *o, int64_t count, PyObject *kind, const void **p, bool optional = false)
+bool vector(const StepCalls *c, PyObject *o, int64_t count, PyObject *kind, const void **p, bool optional = false)
 {
     *p = nullptr;
     if (o == Py_None) return optional;
     int64_t size, step;
     void *at;
-    if (!of_kind(o, kind) || !is_true(o, g_is_cuda) || !layout(o, 1, &size, &step) || size != count || (step != 1 && size > 1) || !tensor(o, &at)) return false;
+    if (!of_kind(o, kind) || !is_here(c, o) || !layout(o, 1, &size, &step) || size != count || (step != 1 && size > 1) || !tensor(o, &at)) return false;
     *p = at;
     return true;
 }
@@ -279,7 +303,7 @@ int matrix(const StepCalls *c, PyObject *o, int64_t *size, int64_t *stride, void
     int k = 0;
     while (k < 3 && c->kinds[k] != kind) ++k;
     Py_XDECREF(kind);
-    if (!kind || k == 3 || !is_true(o, g_is_cuda) || !layout(o, 2, size, step) || (step[1] != 1 && size[1] > 1) || !tensor(o, p)) return -1;
+    if (!kind || k == 3 || !is_here(c, o) || !layout(o, 2, size, step) || (step[1] != 1 && size[1] > 1) || !tensor(o, p)) return -1;
     *stride = size[0] > 1 || step[0] > size[1] ? step[0] : size[1];
     return k;
 }
@@ -298,7 +322,7 @@ bool logits_of(const StepCalls *c, PyObject *logits, PyObject *labels, PyObject 
     x->logits = at;
     x->rows = size[0];
     x->vocab = size[1];
-    return vector(labels, size[0], c->int64, &x->labels) && number(temperature, &x->temperature);
+    return vector(c, labels, size[0], c->int64, &x->labels) && number(temperature, &x->temperature);
 }
 // (handle, logits, labels, log-probabilities, temperature, the stream's callable)
 PyObject *token_logp(PyObject *self, PyObject *const *a, Py_ssize_t n)
@@ -307,7 +331,7 @@ PyObject *token_logp(PyObject *self, PyObject *const *a, Py_ssize_t n)
     void *handle, *stream;
     const void *logp;
     Logits x;
-    if (n != 6 || !address(a[0], &handle) || !logits_of(c, a[1], a[2], a[4], &x) || !vector(a[3], x.rows, c->kinds[0], &logp) || !stream_of(a[5], &stream)) return other();
+    if (n != 6 || !address(a[0], &handle) || !logits_of(c, a[1], a[2], a[4], &x) || !vector(c, a[3], x.rows, c->kinds[0], &logp) || !stream_here(c, a[5], &stream)) return other();
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = c->token_logp(handle, &x, const_cast<void *>(logp), stream);
@@ -324,10 +348,10 @@ PyObject *policy_loss(PyObject *self, PyObject *const *a, Py_ssize_t n)
     Logits x;
     Policy p;
     PyObject *f32 = c->kinds[0];
-    if (n != 16 || !address(a[0], &handle) || !logits_of(c, a[1], a[2], a[10], &x) || !vector(a[3], x.rows, f32, &p.old_logp) ||
-        !vector(a[4], x.rows, f32, &p.advantages) || !vector(a[5], x.rows, f32, &p.weights, true) || !vector(a[6], x.rows, f32, &p.ref_logp, true) ||
+    if (n != 16 || !address(a[0], &handle) || !logits_of(c, a[1], a[2], a[10], &x) || !vector(c, a[3], x.rows, f32, &p.old_logp) ||
+        !vector(c, a[4], x.rows, f32, &p.advantages) || !vector(c, a[5], x.rows, f32, &p.weights, true) || !vector(c, a[6], x.rows, f32, &p.ref_logp, true) ||
         !number(a[7], &p.clip_low) || !number(a[8], &p.clip_high) || !number(a[9], &p.kl_coef) || !number(a[11], &p.grad_scale) ||
-        !vector(a[12], 8, f32, &sums) || !vector(a[13], x.rows, f32, &logp, true)) return other();
+        !vector(c, a[12], 8, f32, &sums) || !vector(c, a[13], x.rows, f32, &logp, true)) return other();
     p.sums = const_cast<void *>(sums);
     p.logp = const_cast<void *>(logp);
     p.dlogits = nullptr;
@@ -336,7 +360,7 @@ PyObject *policy_loss(PyObject *self, PyObject *const *a, Py_ssize_t n)
         int64_t size[2];
         if (matrix(c, a[14], size, &p.dlogits_stride, &p.dlogits) != x.dtype || size[0] != x.rows || size[1] != x.vocab) return other();
     }
-    if (!stream_of(a[15], &stream)) return other();
+    if (!stream_here(c, a[15], &stream)) return other();
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = c->policy_loss(handle, &x, &p, stream);
@@ -350,7 +374,7 @@ PyObject *norm_by(PyObject *self, PyObject *const *a, Py_ssize_t n, bool clip)
     void *handle, *stream;
     const void *out;
     float scale, most;
-    if (n != 5 || !address(a[0], &handle) || !number(a[1], &scale) || !number(a[2], &most) || !vector(a[3], 2, c->kinds[0], &out) || !stream_of(a[4], &stream)) return other();
+    if (n != 5 || !address(a[0], &handle) || !number(a[1], &scale) || !number(a[2], &most) || !vector(c, a[3], 2, c->kinds[0], &out) || !stream_here(c, a[4], &stream)) return other();
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = (clip ? c->grad_clip : c->grad_norm)(handle, scale, most, const_cast<void *>(out), stream);
@@ -374,7 +398,7 @@ PyObject *adamw(PyObject *self, PyObject *const *a, Py_ssize_t n)
         if (!PyFloat_CheckExact(a[2 + k])) return other();
         *at[k] = PyFloat_AS_DOUBLE(a[2 + k]);
     }
-    if (!vector(a[7], 1, c->kinds[0], &coef, true) || !stream_of(a[8], &stream)) return other();
+    if (!vector(c, a[7], 1, c->kinds[0], &coef, true) || !stream_here(c, a[8], &stream)) return other();
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = c->adamw(handle, &w, coef, stream);
@@ -392,12 +416,32 @@ PyObject *step_calls_new(PyTypeObject *type, PyObject *args, PyObject *)
     for (PyObject *k : kinds) Py_INCREF(k);
     for (int k = 0; k < 3; ++k) c->kinds[k] = kinds[k];
     c->int64 = kinds[3];
+    c->device = -1;
     c->token_logp = (token_logp_fn)(uintptr_t)at[0];
     c->policy_loss = (policy_loss_fn)(uintptr_t)at[1];
     c->grad_norm = (grad_norm_fn)(uintptr_t)at[2];
     c->grad_clip = (grad_norm_fn)(uintptr_t)at[3];
     c->adamw = (adamw_fn)(uintptr_t)at[4];
     return reinterpret_cast<PyObject *>(c);
+}
+// the same for the device of this index
+PyObject *on(PyObject *self, PyObject *index)
+{
+    const long device = PyLong_AsLong(index);
+    if (device == -1 && PyErr_Occurred()) return nullptr;
+    PyObject *copy = Py_TYPE(self)->tp_alloc(Py_TYPE(self), 0);
+    if (!copy) return nullptr;
+    StepCalls *c = reinterpret_cast<StepCalls *>(copy);
+    const StepCalls *from = reinterpret_cast<const StepCalls *>(self);
+    for (int k = 0; k < 3; ++k) Py_INCREF(c->kinds[k] = from->kinds[k]);
+    Py_INCREF(c->int64 = from->int64);
+    c->device = device;
+    c->token_logp = from->token_logp;
+    c->policy_loss = from->policy_loss;
+    c->grad_norm = from->grad_norm;
+    c->grad_clip = from->grad_clip;
+    c->adamw = from->adamw;
+    return copy;
 }
 void step_calls_gone(PyObject *self)
 {
@@ -409,7 +453,7 @@ void step_calls_gone(PyObject *self)
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef calls_methods[] = {FAST(compress), FAST(compress_static), FAST(decompress), FAST(compress_groups), FAST(decompress_groups), {nullptr, nullptr, 0, nullptr}};
-PyMethodDef step_calls_methods[] = {FAST(token_logp), FAST(policy_loss), FAST(grad_norm), FAST(grad_clip), FAST(adamw), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef step_calls_methods[] = {FAST(token_logp), FAST(policy_loss), FAST(grad_norm), FAST(grad_clip), FAST(adamw), {"on", on, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyTypeObject CallsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 PyTypeObject StepCallsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 PyTypeObject RawStreamType = {PyVarObject_HEAD_INIT(nullptr, 0)};
@@ -419,7 +463,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", "The hot calls of the 
 
 PyMODINIT_FUNC PyInit__fastcall(void)
 {
-    const struct { PyObject **at; const char *name; } names[] = {{&g_data_ptr, "data_ptr"}, {&g_dtype, "dtype"}, {&g_is_cuda, "is_cuda"}, {&g_shape, "shape"}, {&g_stride, "stride"}};
+    const struct { PyObject **at; const char *name; } names[] = {{&g_data_ptr, "data_ptr"}, {&g_dtype, "dtype"}, {&g_is_cuda, "is_cuda"}, {&g_get_device, "get_device"}, {&g_shape, "shape"}, {&g_stride, "stride"}};
     for (const auto &n : names) if (!*n.at && !(*n.at = PyUnicode_InternFromString(n.name))) return nullptr;
     CallsType.tp_name = "_fastcall.Calls";
     CallsType.tp_basicsize = sizeof(Calls);

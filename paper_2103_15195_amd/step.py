@@ -74,6 +74,9 @@ class _NoFastCalls:
         return None
     policy_loss = grad_norm = grad_clip = adamw = token_logp
 
+    def on(self, device):
+        return self
+
 
 def dtype_id(dtype) -> int:
     """mc_dtype of a torch dtype or its name; None: no type."""
@@ -88,23 +91,31 @@ def dtype_id(dtype) -> int:
 _F32, _I64 = torch.float32, torch.int64
 
 
-def _vector(tensor, name: str, count: int, kind=_F32) -> int:
-    """The address of a contiguous device tensor of `count` elements."""
-    if tensor.dtype is not kind or tensor.numel() != count or not tensor.is_cuda or not tensor.is_contiguous():
-        raise ValueError(f"{name}: {count} contiguous values of {kind} on the device, not {tuple(tensor.shape)} of {tensor.dtype} on {tensor.device}")
+def _vector(tensor, name: str, count: int, device, kind=_F32) -> int:
+    """The address of a contiguous tensor of `count` elements on the handle's device."""
+    if tensor.dtype is not kind or tensor.numel() != count or tensor.device != device or not tensor.is_contiguous():
+        raise ValueError(f"{name}: {count} contiguous values of {kind} on {device}, not {tuple(tensor.shape)} of {tensor.dtype} on {tensor.device}")
     return tensor.data_ptr()
 
 
-def _rows(x, name: str):
-    """(rows, columns, elements from row to row) of a two-dimensional tensor whose rows are contiguous."""
+def _rows(x, name: str, device=None):
+    """(rows, columns, elements from row to row) of a two-dimensional tensor whose rows are contiguous, on the handle's device (None: on any)."""
     shape, step = x.shape, x.stride()
-    if len(shape) != 2 or not x.is_cuda or x.dtype not in DTYPE_IDS or (step[1] != 1 and shape[1] > 1):
-        raise ValueError(f"{name}: rows of contiguous values on the device, of {', '.join(map(str, DTYPE_IDS))}, not {tuple(shape)} of {x.dtype} on {x.device}")
+    if len(shape) != 2 or not (x.is_cuda if device is None else x.device == device) or x.dtype not in DTYPE_IDS or (step[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{name}: rows of contiguous values on {device or 'the device'}, of {', '.join(map(str, DTYPE_IDS))}, not {tuple(shape)} of {x.dtype} on {x.device}")
     return shape[0], shape[1], step[0] if shape[0] > 1 else max(step[0], shape[1])
 
 
+def _stream_on(stream, device) -> Optional[int]:
+    """The stream's handle; None: torch's current stream, for which the handle's device has to be the current one."""
+    at = torch.device("cuda", torch.cuda.current_device()) if stream is None else stream.device if hasattr(stream, "cuda_stream") else device
+    if at != device:
+        raise ValueError(f"{'the current device' if stream is None else 'stream'}: {at}, but the handle was made on {device}")
+    return B._stream_handle(stream)
+
+
 class Step:
-    """One model's list of tensors on the current device: wraps mc_step.
+    """One model's list of tensors on the current device: wraps mc_step.  All that is handed over later has to be on that device.
 
     grad_dtype   type of the gradients (and of what mc_grad_clip writes)
     model_dtype  type of the copy of the weights that the model computes with, or None for no such copy
@@ -127,8 +138,8 @@ class Step:
         nd = None if no_decay is None else (C.c_uint8 * max(n, 1))(*[1 if x else 0 for x in no_decay])
         B._check(lib().mc_step_create(C.byref(self._h), nm, n, self.dtypes["grads"], self.dtypes["model"], nd), "mc_step_create")
         self._at = self._h.value
-        self._fast = lib().fast_step
         self._device = torch.device("cuda", torch.cuda.current_device())
+        self._fast = lib().fast_step.on(self._device.index)
 
     def close(self) -> None:
         if getattr(self, "_h", None):
@@ -157,15 +168,16 @@ class Step:
             for i, (t, n) in enumerate(zip(tensors, self.numel)):
                 if t.numel() != n or not t.is_contiguous() or t.device != self._device or DTYPE_IDS.get(t.dtype) != self.dtypes[name]:
                     raise ValueError(f"{name}[{i}]: {n} contiguous elements of the list's type on {self._device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+        handle = _stream_on(stream, self._device)
         for name, tensors in lists.items():
-            B._check(lib().mc_step_bind(self._h, LISTS[name], B.ptr_array(tensors), B._stream_handle(stream)), "mc_step_bind")
+            B._check(lib().mc_step_bind(self._h, LISTS[name], B.ptr_array(tensors), handle), "mc_step_bind")
             self._kept[name] = tensors
 
     def mc_grad_norm(self, max_norm: float, out, scale: float = 1.0, stream=None) -> None:
         """out: two floats on the device, the norm of scale * gradients and the coefficient that clips them to max_norm."""
         rc = self._fast.grad_norm(self._at, scale, max_norm, out, B._raw_stream) if stream is None else None
         if rc is None:
-            rc = lib().mc_grad_norm(self._h, scale, max_norm, _vector(out, "out", 2), B._stream_handle(stream))
+            rc = lib().mc_grad_norm(self._h, scale, max_norm, _vector(out, "out", 2, self._device), _stream_on(stream, self._device))
         if rc:
             raise B.McError(rc, "mc_grad_norm")
 
@@ -173,7 +185,7 @@ class Step:
         """mc_grad_norm, and the gradients times the coefficient into the list `clipped`, or in place where it is not bound."""
         rc = self._fast.grad_clip(self._at, scale, max_norm, out, B._raw_stream) if stream is None else None
         if rc is None:
-            rc = lib().mc_grad_clip(self._h, scale, max_norm, _vector(out, "out", 2), B._stream_handle(stream))
+            rc = lib().mc_grad_clip(self._h, scale, max_norm, _vector(out, "out", 2, self._device), _stream_on(stream, self._device))
         if rc:
             raise B.McError(rc, "mc_grad_clip")
 
@@ -183,20 +195,21 @@ class Step:
         rc = self._fast.adamw(self._at, step, lr, betas[0], betas[1], eps, weight_decay, coef, B._raw_stream) if stream is None else None
         if rc is None:
             cfg = McAdamwConfig(lr, betas[0], betas[1], eps, weight_decay, step)
-            rc = lib().mc_adamw(self._h, C.byref(cfg), None if coef is None else _vector(coef, "coef", 1), B._stream_handle(stream))
+            rc = lib().mc_adamw(self._h, C.byref(cfg), None if coef is None else _vector(coef, "coef", 1, self._device), _stream_on(stream, self._device))
         if rc:
             raise B.McError(rc, "mc_adamw")
 
 
 class PolicyLoss:
-    """Scratch of the calls over rows of logits, on the current device: wraps mc_loss."""
+    """Scratch of the calls over rows of logits, on the current device, where their tensors have to be: wraps mc_loss."""
 
     def __init__(self):
         self._h = C.c_void_p()
         self._at = 0                             # the same as an int
         B._check(lib().mc_loss_create(C.byref(self._h)), "mc_loss_create")
         self._at = self._h.value
-        self._fast = lib().fast_step
+        self._device = torch.device("cuda", torch.cuda.current_device())
+        self._fast = lib().fast_step.on(self._device.index)
 
     def close(self) -> None:
         if getattr(self, "_h", None):
@@ -214,9 +227,9 @@ class PolicyLoss:
         """logp[r] = log-probability of labels[r] under logits[r] / temperature; 0 where the label is none of the row's."""
         rc = self._fast.token_logp(self._at, logits, labels, logp, temperature, B._raw_stream) if stream is None else None
         if rc is None:
-            rows, vocab, stride = _rows(logits, "logits")
-            x = McLogits(logits.data_ptr(), _vector(labels, "labels", rows, _I64), rows, vocab, stride, DTYPE_IDS[logits.dtype], temperature)
-            rc = lib().mc_token_logp(self._h, C.byref(x), _vector(logp, "logp", rows), B._stream_handle(stream))
+            rows, vocab, stride = _rows(logits, "logits", self._device)
+            x = McLogits(logits.data_ptr(), _vector(labels, "labels", rows, self._device, _I64), rows, vocab, stride, DTYPE_IDS[logits.dtype], temperature)
+            rc = lib().mc_token_logp(self._h, C.byref(x), _vector(logp, "logp", rows, self._device), _stream_on(stream, self._device))
         if rc:
             raise B.McError(rc, "mc_token_logp")
 
@@ -229,21 +242,21 @@ class PolicyLoss:
                                     grad_scale, sums, logp, dlogits, B._raw_stream) if stream is None else None
         if rc is None:
             rc = self._policy_loss(logits, labels, old_logp, advantages, sums, weights, ref_logp, clip, kl_coef, temperature, grad_scale, logp,
-                                   dlogits, B._stream_handle(stream))
+                                   dlogits, _stream_on(stream, self._device))
         if rc:
             raise B.McError(rc, "mc_policy_loss")
 
     def _policy_loss(self, logits, labels, old_logp, advantages, sums, weights, ref_logp, clip, kl_coef, temperature, grad_scale, logp, dlogits, stream) -> int:
         """The same through ctypes, which says what is wrong with an argument."""
-        rows, vocab, stride = _rows(logits, "logits")
-        x = McLogits(logits.data_ptr(), _vector(labels, "labels", rows, _I64), rows, vocab, stride, DTYPE_IDS[logits.dtype], temperature)
+        rows, vocab, stride = _rows(logits, "logits", self._device)
+        x = McLogits(logits.data_ptr(), _vector(labels, "labels", rows, self._device, _I64), rows, vocab, stride, DTYPE_IDS[logits.dtype], temperature)
         slopes, dstride = None, 0
         if dlogits is not None:
-            drows, dvocab, dstride = _rows(dlogits, "dlogits")
+            drows, dvocab, dstride = _rows(dlogits, "dlogits", self._device)
             if drows != rows or dvocab != vocab or dlogits.dtype is not logits.dtype:
                 raise ValueError(f"dlogits: the logits' shape and type, not {tuple(dlogits.shape)} of {dlogits.dtype}")
             slopes = dlogits.data_ptr()
-        p = McPolicy(_vector(old_logp, "old_logp", rows), _vector(advantages, "advantages", rows),
-                     None if weights is None else _vector(weights, "weights", rows), None if ref_logp is None else _vector(ref_logp, "ref_logp", rows),
-                     clip[0], clip[1], kl_coef, grad_scale, _vector(sums, "sums", 8), None if logp is None else _vector(logp, "logp", rows), slopes, dstride)
+        p = McPolicy(_vector(old_logp, "old_logp", rows, self._device), _vector(advantages, "advantages", rows, self._device),
+                     None if weights is None else _vector(weights, "weights", rows, self._device), None if ref_logp is None else _vector(ref_logp, "ref_logp", rows, self._device),
+                     clip[0], clip[1], kl_coef, grad_scale, _vector(sums, "sums", 8, self._device), None if logp is None else _vector(logp, "logp", rows, self._device), slopes, dstride)
         return lib().mc_policy_loss(self._h, C.byref(x), C.byref(p), stream)
