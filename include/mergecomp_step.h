@@ -94,7 +94,7 @@ int mc_grad_clip(mc_step *h, float scale, float max_norm, float *out, void *stre
  * and the model's copy, if the handle has one, is p rounded to its type.
  *   coef    device, one float (such as mc_grad_norm's out + 1), or NULL for 1.  0: the update is left out, nothing is written.
  * Errors: MC_ERR_INVALID_ARG (null, lists not bound, step < 1, betas outside [0, 1), eps <= 0, lr or weight_decay
- * negative or not finite).
+ * negative or not finite, eps 0 or infinite in binary32, the factors 1 - lr weight_decay or lr / (1 - beta1^step) infinite there).
  */
 typedef struct {
     double lr, beta1, beta2, eps, weight_decay;

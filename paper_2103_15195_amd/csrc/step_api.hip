@@ -222,6 +222,8 @@ int mc_adamw(mc_step *h, const mc_adamw_config *c, const float *coef, void *stre
     a.rate = (float)(c->lr / (1.0 - std::pow(c->beta1, (double)c->step)));
     a.root = (float)(1.0 / std::sqrt(1.0 - std::pow(c->beta2, (double)c->step)));
     a.eps = (float)c->eps;
+    // (an eps of 0 there would make 0 / 0 of what has never had a gradient, an infinite rate 0 * infinity)
+    if (!(a.eps > 0.0f) || !std::isfinite(a.eps) || !std::isfinite(a.decay) || !std::isfinite(a.rate) || !std::isfinite(a.root)) return MC_ERR_INVALID_ARG;
     launch_adamw(on(stream), h->grad_dtype, h->model_dtype, view(h), a);
     return launched();
 }
