@@ -78,8 +78,9 @@ int mc_step_bind(mc_step *h, int32_t list, const void *const *ptrs, void *stream
  *   scale      what a gradient is multiplied by before anything else (1 / loss scale, 1 / accumulated steps); finite, > 0
  *   max_norm   > 0; infinity: nothing is clipped
  *   out        device, two floats: norm, coef
- * Squares are summed in binary64, so that neither large nor small gradients are lost.  (A finite norm beyond binary32 is
- * written as infinity; its coef is right.)
+ * Squares are summed in binary64, so that neither large nor small gradients are lost.  A finite norm beyond binary32 is
+ * written as infinity; its coef follows from the norm as it is, rounded to binary32: below 2^-126 it has fewer digits, below 2^-150
+ * it is 0 and so stands for a step that is left out.
  */
 int mc_grad_norm(mc_step *h, float scale, float max_norm, float *out, void *stream);
 

@@ -141,8 +141,8 @@ __device__ __forceinline__ Term left_term(const Term *from)
     return t;
 }
 // By all of a block's threads, behind their rows: the last block adds up the terms of all.  In launches of at most so many threads over at most so many
-// rows.  (So and by a kernel behind, us: 600 x 8000 bf16 8.5 and 11.8, 4096 x 1000 10.2 and 11.8, 512 x 32000 14.1 and 14.6, 2048 x 8000 15.1 and 15.2; beyond the
-// lines 1024 x 32000 25.9 and 23.9, 8192 x 1000 15.2 and 12.4, 16384 x 100 17.1 and 11.7.)
+// rows.  (So and by a kernel behind, us: 600 x 8000 bf16 8.9 and 12.0, 4096 x 1000 10.3 and 12.0, 512 x 32000 14.4 and 14.8; beyond the
+// lines 1024 x 32000 25.8 and 23.7, 1024 x 16000 17.6 and 16.3, 8192 x 1000 15.3 and 12.5, 16384 x 100 17.2 and 12.1, but 2048 x 8000 15.6 and 16.0.)
 constexpr uint64_t kFewThreads = 1u << 19;
 constexpr uint32_t kFewRows = 4096;
 static bool sums_here(const LossArgs &a, uint32_t blocks, uint32_t threads) { return (uint64_t)blocks * threads <= kFewThreads && a.rows <= kFewRows && !a.more; }
@@ -675,14 +675,15 @@ template <class T, bool LOSS>
 static bool loss_of(const LaunchCtx &lc, LossArgs a)
 {
     a.line = kLine;
-    // (a row that would need twice the registers for it is not moved to a line)
+    // (A row that would need twice the registers for it, or the next of the forms below, is not moved to a line.  1536 and 3072 are limits of the policy loss
+    // alone; the log-probabilities go by the same list.)
     const uint32_t close = reach<T>(a, 16u);
     uint32_t vecs = reach<T>(a, kLine);
     for (uint32_t room : {16u, 32u, 64u, 128u, 256u, 384u, 512u, 768u, 1024u, 1536u, 2048u, 3072u, 4096u, 8192u, 16384u}) if (close <= room && room < vecs) { a.line = 16u; vecs = close; }
-    // Few long rows are shared by blocks.  (Policy loss so and with a block to each, us: rows of 128256 bf16, 1 / 64 / 128 / 200 of them 13.6 / 14.0 / 19.0 / 27.5
-    // and 18.2 / 21.0 / 21.7 / 23.7; of 262144 fp32 13.6 / 30.8 / 56.9 / 88.3 and 42.9 / 51.6 / 71.0 / 97.0; of 70000 bf16, 64 / 128 / 200 13.1 / 15.1 / 17.6 and
-    // 17.1 / 17.6 / 18.3.  Below 8192 vectors the second launch costs more than it gains: 1 / 64 of 64000 bf16 13.5 / 13.3 and 11.8 / 14.0, their
-    // log-probabilities alone 8.6 / 8.7 and 6.3 / 7.4.)
+    // Few long rows are shared by blocks.  (Policy loss so and with a block to each, us: rows of 128256 bf16, 1 / 64 / 128 / 200 of them 11.4 / 14.0 / 19.1 / 27.0
+    // and 19.3 / 21.6 / 22.3 / 24.2; of 262144 fp32 11.4 / 30.3 / 56.8 / 87.9 and 43.5 / 52.2 / 69.8 / 95.8; of 70000 bf16, 64 / 128 / 200 11.6 / 15.0 / 17.6 and
+    // 17.9 / 18.1 / 19.0.  Below 8192 vectors the gain is no more than what the host takes for a second launch, which is from 0.5 to 2 us from one machine to another:
+    // 1 / 64 of 64000 bf16 11.3 / 11.0 and 12.2 / 14.5, on a slower host 13.5 / 13.3 and 11.8 / 14.0; their log-probabilities alone 7.8 / 7.6 and 6.3 / 7.4.)
     const uint32_t parts = (reach<T>(a, kLine) + kPartVecs - 1u) / kPartVecs;
     if (a.rows <= kPartRows && parts <= kMostParts && vecs > 1024 * 8 && !a.more) {
         a.line = kLine;
