@@ -14,6 +14,8 @@
  *   - those of mergecomp.h: pointers are "host" or "device" as stated, calls only enqueue kernels on the caller's stream
  *     (void* = hipStream_t), allocate nothing, never synchronise and read nothing back; all calls on one handle must be
  *     issued in stream order, since its scratch is shared between them.  0 or a negative mc_status; no call throws or aborts.
+ *   - A handle belongs to the device that was current when it was made: its calls take memory of that device and a stream of it (NULL:
+ *     the current device's, which has to be that one).
  *   - Arithmetic is binary32; sums over tensors and over rows are binary64.  Sums are taken in an order that depends on sizes, on where
  *     rows and tensors begin in a cache line, and on the device alone: the same call gives the same bits.  Values of 16
  *     bits are widened when they are read and rounded once, to nearest even, when they are written.
