@@ -12,7 +12,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmergecomp.so")
 FASTCALL = os.path.join(HERE, "_fastcall" + sysconfig.get_config_var("EXT_SUFFIX"))      # (other interpreters' layouts differ: none but this one loads it)
-SOURCES = ["mc_api.hip", "kernels_dense.hip", "kernels_sparse.hip", "step_api.hip", "kernels_step.hip", "kernels_loss.hip"]
+SOURCES = ["mc_api.hip", "kernels_dense.hip", "kernels_sparse.hip", "step_api.hip", "kernels_step.hip", "kernels_loss.hip",
+           "mx_api.hip", "kernels_adamw8.hip", "kernels_mx_quantize.hip", "kernels_mx_matmul.hip"]
 
 # -ffp-contract=off: the residual updates must round every fp32 operation on its own
 # (no fused multiply-add), or codes and residuals would not be reproducible bit for bit.

@@ -1,0 +1,156 @@
+// AdamW with moments in 8 bits.
+//
+// A stream, like AdamW in 32 bits, of 16 bytes an element instead of 28.  A thread has eight consecutive elements, so that a block of
+// 128 that shares a scale is a row of 16 lanes, whose largest magnitude is found without LDS.
+#include "mx_internal.h"
+
+namespace mc {
+
+// The largest of each row of 16 lanes, in all of them.
+template <int ROTATE>
+__device__ __forceinline__ float rotated_max(float x)
+{
+    const float y = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + ROTATE, 0xf, 0xf, false));
+    return fmaxf(x, y);
+}
+__device__ __forceinline__ float row_max(float x)
+{
+    return rotated_max<1>(rotated_max<2>(rotated_max<4>(rotated_max<8>(x))));
+}
+
+typedef uint32_t codes8 __attribute__((ext_vector_type(2)));
+typedef codes8 codes8_any __attribute__((aligned(1)));
+typedef float float2v __attribute__((ext_vector_type(2)));
+// Eight elements' codes, as values without their scale.
+__device__ __forceinline__ codes8 load_codes(global_ptr<const uint8_t> p, int32_t i, int32_t hi)
+{
+    if (i + 8 <= hi) return __builtin_nontemporal_load((global_ptr<const codes8_any>)(p + i));
+    codes8 c = {0u, 0u};
+    for (int e = 0; e < 8; ++e) if (i + e < hi) c[e / 4] |= (uint32_t)p[i + e] << (8 * (e % 4));
+    return c;
+}
+__device__ __forceinline__ void store_codes(global_ptr<uint8_t> p, int32_t i, int32_t hi, codes8 c)
+{
+    if (i + 8 <= hi) __builtin_nontemporal_store(c, (global_ptr<codes8_any>)(p + i));
+    else for (int e = 0; e < 8; ++e) if (i + e < hi) p[i + e] = (uint8_t)(c[e / 4] >> (8 * (e % 4)));
+}
+__device__ __forceinline__ void held(codes8 c, float scale, float (&x)[8])
+{
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const float2v lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[k], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[k], true);
+        x[4 * k] = lo[0] * scale; x[4 * k + 1] = lo[1] * scale; x[4 * k + 2] = hi[0] * scale; x[4 * k + 3] = hi[1] * scale;
+    }
+}
+// Values to codes under the largest finite magnitude of their block; returns the scale.  A NaN stays one, an infinity becomes one (the conversion
+// has no infinity, and rounds what is up to half a step above 448 to 448, which the quotient's own rounding needs).
+template <bool ROOT>
+__device__ __forceinline__ float hold8(const float (&x)[8], codes8 &c)
+{
+    float top = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float a = fabsf(x[e]);
+        top = fmaxf(top, a < __builtin_huge_valf() ? a : 0.0f);
+    }
+    top = row_max(top);
+    const float scale = top >= 0x1p-100f ? top * (1.0f / 448.0f) : 0.0f, back = scale > 0.0f ? 1.0f / scale : 0.0f;
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        y[e] = x[e] * back;
+        if (ROOT) y[e] = x[e] > 0.0f && scale > 0.0f ? fmaxf(y[e], 0x1p-9f) : y[e];        // (not of a NaN, which is above nothing)
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k], y[4 * k + 1], 0, false);
+        c[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k + 2], y[4 * k + 3], lo, true);
+    }
+    return scale;
+}
+
+struct NoCopy8 {};
+template <class T>
+__device__ __forceinline__ global_ptr<T> list8(const Step8View &v, uint32_t list, uint32_t tensor)
+{
+    return in_global(reinterpret_cast<T *>(ld_uniform(v.addr + (size_t)list * v.tensors + tensor)));
+}
+template <class T>
+__device__ __forceinline__ void load8(global_ptr<const T> p, int32_t i, int32_t hi, float (&x)[8])
+{
+    if constexpr (sizeof(T) == 2) load_some<8, T>(p, i, 0, hi, x);
+    else {
+        float lo[4], up[4];
+        load_some<4, T>(p, i, 0, hi, lo);
+        load_some<4, T>(p, i + 4, 0, hi, up);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { x[e] = lo[e]; x[4 + e] = up[e]; }
+    }
+}
+template <class T>
+__device__ __forceinline__ void store8(global_ptr<T> p, int32_t i, int32_t hi, const float (&x)[8])
+{
+    if constexpr (sizeof(T) == 2) store_some<8, T>(p, i, 0, hi, x);
+    else {
+        const float lo[4] = {x[0], x[1], x[2], x[3]}, up[4] = {x[4], x[5], x[6], x[7]};
+        store_some<4, T>(p, i, 0, hi, lo);
+        store_some<4, T>(p, i + 4, 0, hi, up);
+    }
+}
+template <class T, class M>
+__global__ __launch_bounds__(kBlock) void adamw8_k(Step8View v, AdamwArgs a)
+{
+    const float coef = a.coef ? ld_uniform(a.coef) : 1.0f;
+    const uint32_t name = ld_uniform(&v.pieces[blockIdx.x].tensor), index = ld_uniform(&v.pieces[blockIdx.x].index), tensor = name & ~kNoDecay;
+    const int32_t hi = ld_uniform(&v.pieces[blockIdx.x].left);
+    const int64_t from = (int64_t)index * kPiece8;
+    const global_ptr<const T> grad = list8<const T>(v, MC_LIST8_GRADS, tensor) + from;
+    const global_ptr<float> param = list8<float>(v, MC_LIST8_PARAMS, tensor) + from;
+    const global_ptr<uint8_t> avg = list8<uint8_t>(v, MC_LIST8_EXP_AVG, tensor) + from, avg_sq = list8<uint8_t>(v, MC_LIST8_EXP_AVG_SQ, tensor) + from;
+    const int64_t first = (int64_t)index * (kPiece8 / kBlock8) + threadIdx.x / (kBlock8 / 8);
+    const global_ptr<float> avg_scale = list8<float>(v, MC_LIST8_EXP_AVG_SCALE, tensor) + first, avg_sq_scale = list8<float>(v, MC_LIST8_EXP_AVG_SQ_SCALE, tensor) + first;
+    const int32_t i = (int32_t)threadIdx.x * 8;
+    const bool mine = (i & ~(int32_t)(kBlock8 - 1)) < hi;                // the block of 128 holds elements
+    const float decay = name & kNoDecay ? 1.0f : a.decay;
+    float g[8], w[8], m[8], r[8];
+    load8<T>(grad, i, hi, g);
+    load8<float>(param, i, hi, w);
+    const codes8 cm = load_codes(avg, i, hi), cr = load_codes(avg_sq, i, hi);
+    const float sm = mine ? *avg_scale : 0.0f, sr = mine ? *avg_sq_scale : 0.0f;
+    if (coef == 0.0f) return;            // (looked at behind the loads, which need not wait for it)
+    held(cm, sm, m);
+    held(cr, sr, r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        g[e] *= coef;
+        m[e] = a.beta1 * m[e] + a.one_minus_beta1 * g[e];
+        r[e] = sqrtf(a.beta2 * (r[e] * r[e]) + a.one_minus_beta2 * (g[e] * g[e]));
+        w[e] = decay * w[e] - a.rate * (m[e] / (r[e] * a.root + a.eps));
+    }
+    store8<float>(param, i, hi, w);
+    if constexpr (!std::is_same_v<M, NoCopy8>) store8<M>(list8<M>(v, MC_LIST8_MODEL, tensor) + from, i, hi, w);
+    codes8 c;
+    const float tm = hold8<false>(m, c);
+    store_codes(avg, i, hi, c);
+    const float tr = hold8<true>(r, c);
+    store_codes(avg_sq, i, hi, c);
+    if (mine && threadIdx.x % (kBlock8 / 8) == 0) {
+        *avg_scale = tm;
+        *avg_sq_scale = tr;
+    }
+}
+
+template <class T>
+static void adamw8_of(const LaunchCtx &lc, int model_dtype, const Step8View &v, const AdamwArgs &a)
+{
+    auto k = model_dtype == MC_DTYPE_NONE ? adamw8_k<T, NoCopy8> : model_dtype == MC_DTYPE_BF16 ? adamw8_k<T, __bf16> : adamw8_k<T, _Float16>;
+    in_launches(v.npieces, [&](uint64_t first, uint32_t n) { launch(k, dim3(n), dim3(kBlock), lc.stream, Step8View{v.pieces + first, v.addr, n, v.tensors}, a); });
+}
+void launch_adamw8(const LaunchCtx &lc, int dtype, int model_dtype, const Step8View &v, const AdamwArgs &a)
+{
+    if (dtype == MC_DTYPE_F32) adamw8_of<float>(lc, model_dtype, v, a);
+    else if (dtype == MC_DTYPE_BF16) adamw8_of<__bf16>(lc, model_dtype, v, a);
+    else adamw8_of<_Float16>(lc, model_dtype, v, a);
+}
+
+}  // namespace mc

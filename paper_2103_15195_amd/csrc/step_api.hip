@@ -4,6 +4,7 @@
 #include <new>
 #include <vector>
 
+#include "host_util.h"
 #include "step_internal.h"
 
 using namespace mc;
@@ -31,79 +32,8 @@ struct mc_loss {
 
 namespace {
 
-bool known(int32_t dtype) { return dtype == MC_DTYPE_F32 || dtype == MC_DTYPE_BF16 || dtype == MC_DTYPE_F16; }
-uintptr_t size_of(int32_t dtype) { return dtype == MC_DTYPE_F32 ? 4u : 2u; }
-bool off(const void *p, uintptr_t align) { return (reinterpret_cast<uintptr_t>(p) & (align - 1u)) != 0; }
-int launched() { return hipGetLastError() == hipSuccess ? MC_OK : MC_ERR_DEVICE; }
-LaunchCtx on(void *stream)
-{
-    (void)hipGetLastError();
-    return LaunchCtx{static_cast<hipStream_t>(stream), nullptr, nullptr, nullptr};
-}
 StepView view(const mc_step *h) { return {h->d_pieces, h->d_addr, h->npieces, (uint32_t)h->live.size()}; }
 bool ready(const mc_step *h, int32_t list) { return h->bound[list] || h->live.empty(); }
-
-struct OnDevice {                         // makes a handle's device current where something is freed
-    int prev = -1;
-    bool switched = false;
-    explicit OnDevice(int device)
-    {
-        if (hipGetDevice(&prev) == hipSuccess && prev != device) switched = hipSetDevice(device) == hipSuccess;
-    }
-    ~OnDevice() { if (switched) (void)hipSetDevice(prev); }
-};
-
-template <class T>
-int grab(T **p, size_t bytes)
-{
-    void *q = nullptr;
-    if (hipMalloc(&q, bytes) != hipSuccess) { (void)hipGetLastError(); return MC_ERR_ALLOC; }
-    *p = static_cast<T *>(q);
-    return MC_OK;
-}
-
-int grab_counts(uint32_t **p)
-{
-    const int rc = grab(p, kArriveBytes);
-    if (rc != MC_OK) return rc;
-    // (done before work on any stream)
-    return hipMemset(*p, 0, kArriveBytes) == hipSuccess && hipDeviceSynchronize() == hipSuccess ? MC_OK : MC_ERR_DEVICE;
-}
-
-// ---- whether two things in memory share a byte
-struct Span {
-    uintptr_t at;
-    uint64_t bytes;
-};
-Span span(const void *p, uint64_t bytes) { return {reinterpret_cast<uintptr_t>(p), p ? bytes : 0u}; }
-bool meet(Span a, Span b) { return a.bytes && b.bytes && a.at < b.at + b.bytes && b.at < a.at + a.bytes; }
-// The rows of a matrix: `rows` of them, `bytes` each (not 0), `step` from one to the next.
-struct RowsAt {
-    uintptr_t at;
-    uint64_t rows, bytes, step;
-    // (a step that no address space holds stands for all longer ones, so that sums of an address and a step stay below 2^64)
-    RowsAt(const void *p, int64_t n, int64_t vocab, int64_t stride, uintptr_t size)
-        : at(reinterpret_cast<uintptr_t>(p)), rows(p ? (uint64_t)n : 0u), bytes((uint64_t)vocab * size), step((uint64_t)(stride < (int64_t(1) << 58) ? stride : int64_t(1) << 58) * size) {}
-    Span all() const { return {at, rows ? (rows > (uint64_t(1) << 62) / step ? uint64_t(1) << 62 : (rows - 1u) * step) + bytes : 0u}; }
-};
-bool meet(Span a, const RowsAt &m)
-{
-    if (!meet(a, m.all())) return false;
-    const uint64_t k = a.at > m.at ? (a.at - m.at) / m.step : 0u;                 // the last row that begins at a or before it, or the first
-    return meet(a, Span{m.at + k * m.step, m.bytes}) || (k + 1u < m.rows && meet(a, Span{m.at + (k + 1u) * m.step, m.bytes}));
-}
-// (of as many rows)
-bool meet(const RowsAt &a, const RowsAt &b)
-{
-    if (!meet(a.all(), b.all())) return false;
-    if (a.step != b.step) {            // (and in one another's reach: no layout that a program would choose)
-        for (uint64_t k = 0; k < a.rows; ++k) if (meet(Span{a.at + k * a.step, a.bytes}, b)) return true;
-        return false;
-    }
-    // rows of one step lie on each other where the distance of the two is closer to a multiple of it than a row is long
-    const uint64_t distance = a.at > b.at ? a.at - b.at : b.at - a.at, k = distance / a.step, behind = distance % a.step;
-    return (k < a.rows && behind < a.bytes) || (k + 1u < a.rows && a.step - behind < a.bytes);
-}
 
 }  // namespace
 
@@ -209,21 +139,10 @@ int mc_grad_clip(mc_step *h, float scale, float max_norm, float *out, void *stre
 
 int mc_adamw(mc_step *h, const mc_adamw_config *c, const float *coef, void *stream)
 {
-    if (!h || !c || off(coef, 4) || c->step < 1) return MC_ERR_INVALID_ARG;
-    if (!(c->beta1 >= 0.0 && c->beta1 < 1.0 && c->beta2 >= 0.0 && c->beta2 < 1.0 && c->eps > 0.0 && std::isfinite(c->eps))) return MC_ERR_INVALID_ARG;
-    if (!(c->lr >= 0.0 && std::isfinite(c->lr) && c->weight_decay >= 0.0 && std::isfinite(c->weight_decay))) return MC_ERR_INVALID_ARG;
+    AdamwArgs a;
+    if (!h || !adamw_args(c, coef, a)) return MC_ERR_INVALID_ARG;
     for (int32_t list : {MC_LIST_GRADS, MC_LIST_PARAMS, MC_LIST_EXP_AVG, MC_LIST_EXP_AVG_SQ}) if (!ready(h, list)) return MC_ERR_INVALID_ARG;
     if (h->model_dtype != MC_DTYPE_NONE && !ready(h, MC_LIST_MODEL)) return MC_ERR_INVALID_ARG;
-    AdamwArgs a;
-    a.coef = coef;
-    a.beta1 = (float)c->beta1; a.one_minus_beta1 = (float)(1.0 - c->beta1);
-    a.beta2 = (float)c->beta2; a.one_minus_beta2 = (float)(1.0 - c->beta2);
-    a.decay = (float)(1.0 - c->lr * c->weight_decay);
-    a.rate = (float)(c->lr / (1.0 - std::pow(c->beta1, (double)c->step)));
-    a.root = (float)(1.0 / std::sqrt(1.0 - std::pow(c->beta2, (double)c->step)));
-    a.eps = (float)c->eps;
-    // (an eps of 0 there would make 0 / 0 of what has never had a gradient, an infinite rate 0 * infinity)
-    if (!(a.eps > 0.0f) || !std::isfinite(a.eps) || !std::isfinite(a.decay) || !std::isfinite(a.rate) || !std::isfinite(a.root)) return MC_ERR_INVALID_ARG;
     launch_adamw(on(stream), h->grad_dtype, h->model_dtype, view(h), a);
     return launched();
 }
@@ -293,8 +212,8 @@ int mc_token_logp(mc_loss *h, const mc_logits *x, float *logp, void *stream)
     const int rc = logits_args(h, x, a);
     if (rc != MC_OK) return rc;
     if ((a.rows && !logp) || off(logp, 4)) return MC_ERR_INVALID_ARG;
-    const Span to = span(logp, 4u * (uint64_t)a.rows);
-    if (meet(to, span(x->labels, 8u * (uint64_t)a.rows)) || meet(to, RowsAt(x->logits, x->rows, x->vocab, x->stride, size_of(x->dtype)))) return MC_ERR_INVALID_ARG;
+    const Extent to = extent(logp, 4u * (uint64_t)a.rows);
+    if (meet(to, extent(x->labels, 8u * (uint64_t)a.rows)) || meet(to, RowsAt(x->logits, x->rows, x->vocab, x->stride, size_of(x->dtype)))) return MC_ERR_INVALID_ARG;
     a.logp = logp;
     launch_token_logp(on(stream), x->dtype, a);
     return launched();
@@ -306,9 +225,9 @@ int mc_token_logp(mc_loss *h, const mc_logits *x, float *logp, void *stream)
 static bool overlaps(const mc_logits *x, const mc_policy *p)
 {
     const uint64_t n = (uint64_t)x->rows;
-    const Span logp = span(p->logp, 4u * n), sums = span(p->sums, 32u);
+    const Extent logp = extent(p->logp, 4u * n), sums = extent(p->sums, 32u);
     const RowsAt logits(x->logits, x->rows, x->vocab, x->stride, size_of(x->dtype)), slopes(p->dlogits, x->rows, x->vocab, p->dlogits_stride, size_of(x->dtype));
-    for (const Span s : {span(x->labels, 8u * n), span(p->old_logp, 4u * n), span(p->advantages, 4u * n), span(p->weights, 4u * n), span(p->ref_logp, 4u * n)})
+    for (const Extent s : {extent(x->labels, 8u * n), extent(p->old_logp, 4u * n), extent(p->advantages, 4u * n), extent(p->weights, 4u * n), extent(p->ref_logp, 4u * n)})
         if (meet(logp, s) || meet(s, slopes) || (n > kTermRows && meet(sums, s))) return true;
     if (meet(logp, sums) || meet(logp, logits) || meet(logp, slopes) || meet(sums, slopes) || (n > kTermRows && meet(sums, logits))) return true;
     return p->dlogits != x->logits && meet(slopes, logits);
