@@ -50,6 +50,7 @@ int mc_step8_destroy(mc_step8 *h);
 /* As mc_step_bind. */
 int mc_step8_bind(mc_step8 *h, int32_t list, const void *const *ptrs, void *stream);
 /* As mc_adamw: the same formulas in binary32 on the values that are held, weights from the new moments before they are rounded.
+ * (A second moment below 2^-126 may count as 0, and what the first is divided by is at least 2^-126.)
  * coef: what mc_grad_norm leaves in out + 1, or NULL for 1; 0: nothing is written. */
 int mc_adamw8(mc_step8 *h, const mc_adamw_config *cfg, const float *coef, void *stream);
 

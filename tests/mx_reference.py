@@ -5,6 +5,7 @@ import numpy as np
 import torch
 
 F64 = torch.float64
+LOST = 2.0 ** -63                 # the root of a second moment that may count as 0, 2^-126
 U = 2.0 ** -24                    # half a unit in the last place of binary32, relative
 GRID = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
 BORDERS = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0])
@@ -45,12 +46,12 @@ def adamw8(p, cm, sm, cr, sr, g, coef, step, lr, betas, eps, decay):
     rate = lr / (1 - b1 ** step)
     p_new = p - lr * decay * p - rate * m_new / den
     # m: a held value is off by U, g by U, each product by two more with its constant, the sum by one; its terms may cancel.  v: squares of
-    # what is off by U by 3 U, with their factors 5 U, the sum 6 U; the root half of that and its own.  p: the quotient has m's
+    # what is off by U by 3 U, with their factors 5 U, the sum 6 U; the root half of that and 2 U of its own (a unit in the last place).  p: the quotient has m's
     # error, the root's, and 6 U of product, sum, quotient and rate; its difference from p's product 4 U.
     size = (b1 * m).abs() + ((1 - b1) * g).abs()
     tiny = 2.0 ** -140
-    off_m, off_r = 5 * U * size + tiny, 5 * U * root + 2.0 ** -70
-    off_p = 4 * U * p.abs() + rate * (20 * U * size + tiny) / den + rate * m_new.abs() / den ** 2 * 2.0 ** -70
+    off_m, off_r = 5 * U * size + tiny, 5 * U * root + LOST
+    off_p = 4 * U * p.abs() + rate * (20 * U * size + tiny) / den + rate * m_new.abs() / den ** 2 * LOST
     return (p_new, m_new, root), (off_p, off_m, off_r)
 
 
