@@ -1,162 +1,293 @@
 // Matrices to microscaled 4-bit floating point.
 //
-// A lane quantises a whole block of 32 values, so that its largest magnitude needs no other lane, and its 16 bytes of codes are one
-// store; lane g * 16 + r has the block g of row r of a tile, which is where the layout has it: a wavefront's codes are 1024 bytes
-// in a row.
+// A stream: what bounds it is the memory's rate.  A lane loads 16 bytes of a row, eight or four elements, so that a row's 128 columns are 16 or 32
+// lanes and a block of 32 four or eight of them, whose largest magnitude takes two or three exchanges between neighbours.  Along the columns a lane
+// holds all 32 rows of its block in registers: no exchange at all, and the rows' blocks are taken from the same registers.
 #include "mx_internal.h"
 
 namespace mc {
 
 typedef uint32_t codes4 __attribute__((ext_vector_type(4)));
-typedef float float2v __attribute__((ext_vector_type(2)));
+typedef uint16_t halves __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+template <class T> constexpr int kHas = 16 / (int)sizeof(T);             // elements of a lane
+template <class T> constexpr uint32_t kRowLanes = kMxStep / kHas<T>;     // lanes to a row's 128 columns
+template <class T> constexpr uint32_t kBlockLanes = kMxBlock / kHas<T>;  // lanes to a block of 32
+
+__device__ __forceinline__ float float_of(uint32_t bits) { return __builtin_bit_cast(float, bits); }
+
+// ---- 16 bytes of a row -----------------------------------------------------------------------------------------------
+template <int SIZE> struct RawOf { typedef codes4 type __attribute__((aligned(2))); };       // on an element's boundary
+template <> struct RawOf<4> { typedef codes4 type __attribute__((aligned(4))); };
+template <class T>
+__device__ __forceinline__ codes4 load_raw(const T *row, uint32_t col, uint32_t cols, bool full)
+{
+    if (full) return *(global_ptr<const typename RawOf<sizeof(T)>::type>)(in_global(row) + col);
+    codes4 w = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < kHas<T>; ++e) {
+        if (col + e >= cols) continue;
+        if constexpr (sizeof(T) == 4) w[e] = __builtin_bit_cast(uint32_t, in_global(row)[col + e]);
+        else w[e / 2] |= (uint32_t)__builtin_bit_cast(uint16_t, in_global(row)[col + e]) << (16 * (e % 2));
+    }
+    return w;
+}
+template <class T>
+__device__ __forceinline__ void store_raw(T *row, uint32_t col, uint32_t cols, codes4 w)
+{
+    if (col + kHas<T> <= cols) {
+        __builtin_nontemporal_store(w, (global_ptr<typename RawOf<sizeof(T)>::type>)(in_global(row) + col));
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < kHas<T>; ++e) {
+        if (col + e >= cols) continue;
+        if constexpr (sizeof(T) == 4) in_global(row)[col + e] = float_of(w[e]);
+        else in_global(row)[col + e] = __builtin_bit_cast(T, (uint16_t)(w[e / 2] >> (16 * (e % 2))));
+    }
+}
+// Magnitudes compare as whole numbers, and so do two of 16 bits in a word.
+template <class T>
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t w)
+{
+    if constexpr (sizeof(T) == 4) {
+        w &= 0x7fffffffu;
+        return a > w ? a : w;
+    } else {
+        const halves x = __builtin_bit_cast(halves, a), y = __builtin_bit_cast(halves, w & 0x7fff7fffu);
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, y));
+    }
+}
+// A magnitude of T's, of 16 bits in the low half, as a 32-bit one's bits.
+template <class T>
+__device__ __forceinline__ uint32_t bits_of(uint32_t a)
+{
+    if constexpr (std::is_same_v<T, __bf16>) return a << 16;
+    else if constexpr (std::is_same_v<T, _Float16>) return __builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(_Float16, (uint16_t)a));
+    else return a;
+}
+// Two elements to codes in byte AT of a word.
+template <class T, int AT>
+__device__ __forceinline__ uint32_t pair_codes(uint32_t old, uint32_t w, float p)
+{
+    if constexpr (std::is_same_v<T, __bf16>) return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, __builtin_bit_cast(bf16x2, w), p, AT);
+    else return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(old, __builtin_bit_cast(f16x2, w), p, AT);
+}
+
+// ---- scales ------------------------------------------------------------------------------------------------------------
 // The scale's byte of a block whose largest magnitude has these bits.  fraction * 2^E with a fraction up to 1.75 gets 2^(E - 2), of which it is up to 7
 // times as much; a larger one 2^(E - 1).  (Of normal values 1.25 percent of the square are lost, with 2^(E - 2) for all 1.32, with 2^(E - 1)
 // wherever 6 would be exceeded 1.33; of uniform ones 0.98, 2.07 and 0.98.)
 __device__ __forceinline__ uint32_t scale_of(uint32_t top)
 {
-    if (top >= 0x7f800000u) return 255u;
-    const int32_t e = (int32_t)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x600000u);
-    return e < 0 ? 0u : (uint32_t)e;
+    const int32_t e = (int32_t)((top + 0x1fffffu) >> 23) - 2;            // (fractions above 1.75 carry)
+    return top >= 0x7f800000u ? 255u : e < 0 ? 0u : (uint32_t)e;
 }
 __device__ __forceinline__ float power_of(uint32_t scale) { return __builtin_bit_cast(float, scale ? scale << 23 : 0x00400000u); }
 
-// 32 values to their codes, and the scale's byte.
-__device__ __forceinline__ codes4 quantised(const float (&x)[32], uint32_t &scale)
+template <int CTRL>
+__device__ __forceinline__ uint32_t neighbour(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, false); }
+constexpr int kOther = 0xB1, kOtherPair = 0x4E, kMirrored = 0x141;       // lane ^ 1, lane ^ 2, lane ^ 7
+// The largest of the lanes that a block of 32 columns is spread over.
+template <class T>
+__device__ __forceinline__ uint32_t block_max(uint32_t x)
 {
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 32; ++e) {
-        const uint32_t a = __builtin_bit_cast(uint32_t, x[e]) & 0x7fffffffu;
-        top = a > top ? a : top;
+    uint32_t y = neighbour<kOther>(x);
+    x = x > y ? x : y;
+    y = neighbour<kOtherPair>(x);
+    x = x > y ? x : y;
+    if constexpr (kBlockLanes<T> == 8) {
+        y = neighbour<kMirrored>(x);
+        x = x > y ? x : y;
     }
-    scale = scale_of(top);
-    codes4 c = {0u, 0u, 0u, 0u};
-    if (scale == 255u) return c;
+    return x;
+}
+
+// ---- a lane's part of a row ----------------------------------------------------------------------------------------------
+// The block's scale, and the lane's codes: 32 bits of eight elements, 16 of four.
+template <class T>
+__device__ __forceinline__ uint32_t row_codes(codes4 w, uint32_t &scale)
+{
+    uint32_t top = larger<T>(larger<T>(larger<T>(larger<T>(0u, w[0]), w[1]), w[2]), w[3]);
+    if constexpr (sizeof(T) == 2) top = (top & 0xffffu) > top >> 16 ? top & 0xffffu : top >> 16;
+    scale = scale_of(block_max<T>(bits_of<T>(top)));
     const float p = power_of(scale);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        uint32_t w = 0;
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[8 * k], x[8 * k + 1], p, 0);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[8 * k + 2], x[8 * k + 3], p, 1);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[8 * k + 4], x[8 * k + 5], p, 2);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[8 * k + 6], x[8 * k + 7], p, 3);
-        c[k] = w;
+    uint32_t c = 0;
+    if constexpr (sizeof(T) == 2) {
+        c = pair_codes<T, 0>(c, w[0], p);
+        c = pair_codes<T, 1>(c, w[1], p);
+        c = pair_codes<T, 2>(c, w[2], p);
+        c = pair_codes<T, 3>(c, w[3], p);
+    } else {
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, float_of(w[0]), float_of(w[1]), p, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, float_of(w[2]), float_of(w[3]), p, 1);
     }
-    return c;
+    return scale == 255u ? 0u : c;
 }
 // What codes stand for, within the range of T.
 template <class T>
-__device__ __forceinline__ void values_of(codes4 c, uint32_t scale, float (&x)[32])
+__device__ __forceinline__ codes4 values_of(uint32_t c, uint32_t scale)
 {
-    const float p = scale == 255u ? __builtin_nanf("") : power_of(scale);
     constexpr float most = std::is_same_v<T, _Float16> ? 65504.0f : std::is_same_v<T, __bf16> ? 0x1.fep127f : 0x1.fffffep127f;
+    const float p = power_of(scale), keep = scale == 255u ? __builtin_nanf("") : 1.0f;
+    const f32x2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, p, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, p, 1),
+                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, p, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, p, 3)};
+    codes4 w;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t code = c[k] >> (4 * e) & 15u, size = code & 7u;
-            // twice the value: 0 1 2 3 4 6 8 12, as a nibble each
-            const float v = (float)(int32_t)(0xC8643210u >> (4 * size) & 15u) * 0.5f * p;
-            const float held = v > most ? most : v;                 // (NaN passes)
-            x[8 * k + e] = code & 8u ? -held : held;
+    for (int k = 0; k < kHas<T> / 2; ++k) {
+        const float a = __builtin_amdgcn_fmed3f(x[k][0], -most, most) * keep, b = __builtin_amdgcn_fmed3f(x[k][1], -most, most) * keep;
+        if constexpr (sizeof(T) == 4) {
+            w[2 * k] = __builtin_bit_cast(uint32_t, a);
+            w[2 * k + 1] = __builtin_bit_cast(uint32_t, b);
+        } else if constexpr (std::is_same_v<T, __bf16>) {
+            w[k] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+        } else {
+            w[k] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
         }
     }
+    return w;
 }
-__device__ __forceinline__ void put(const MxView &m, uint32_t tile, uint32_t step, uint32_t lane, codes4 c, uint32_t scale)
+__device__ __forceinline__ size_t codes_at(const MxView &m, uint32_t row, uint32_t step, uint32_t group)
 {
-    *(global_ptr<codes4>)(in_global(m.codes) + ((size_t)tile * m.steps + step) * kMxCodes + lane * 16u) = c;
-    in_global(m.scales)[(((size_t)(tile / 4u) * m.steps + step) * 64u + lane) * 4u + tile % 4u] = (uint8_t)scale;
+    return (((size_t)(row / 16u) * m.steps + step) * 64u + group * 16u + row % 16u) * 16u;
 }
-template <class T, int N>
-__device__ __forceinline__ void load_row(const T *row, int32_t from, int32_t cols, float (&x)[32])
+__device__ __forceinline__ size_t scales_at(const MxView &m, uint32_t row, uint32_t step, uint32_t group)
 {
-#pragma unroll
-    for (int k = 0; k < 32 / N; ++k) {
-        float y[N];
-        load_some<N, T, false>(in_global(row), from + N * k, 0, cols, y);
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[N * k + e] = y[e];
-    }
+    return (((size_t)(row / 64u) * m.steps + step) * 64u + group * 16u + row % 16u) * 4u;
 }
-template <class T, int N>
-__device__ __forceinline__ void store_row(T *row, int32_t from, int32_t cols, const float (&x)[32])
+// A lane's codes of one row; `lane`: its place in the row.
+template <class T>
+__device__ __forceinline__ void put_codes(const MxView &m, uint32_t row, uint32_t step, uint32_t lane, uint32_t c)
 {
-#pragma unroll
-    for (int k = 0; k < 32 / N; ++k) {
-        float y[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) y[e] = x[N * k + e];
-        store_some<N, T>(in_global(row), from + N * k, 0, cols, y);
-    }
+    const global_ptr<uint8_t> to = in_global(m.codes) + codes_at(m, row, step, lane / kBlockLanes<T>) + lane % kBlockLanes<T> * (16u / kBlockLanes<T>);
+    if constexpr (sizeof(T) == 2) *(global_ptr<uint32_t>)to = c;
+    else *(global_ptr<uint16_t>)to = (uint16_t)c;
 }
 
-// Along the rows: a wavefront to a tile of 16 rows by 128 columns.
+// ---- along the rows ----------------------------------------------------------------------------------------------------
+// 64 rows by 128 columns to a block.  A thread has the same columns of the same row of each of the four tiles of 16 rows (of 32-bit values: of two rows),
+// so that it has a word of scales together.
 template <class T, bool VALUES>
-__global__ __launch_bounds__(kBlock) void mx_rows_k(MxSource s, uint64_t first, uint64_t tiles)
+__global__ __launch_bounds__(kBlock) void mx_rows_k(MxSource s, uint64_t first, uint32_t steps)
 {
-    constexpr int N = 16 / (int)sizeof(T);
-    const uint64_t t = (first + blockIdx.x) * (kBlock / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (t >= tiles) return;
-    const uint32_t steps = (s.cols + kMxStep - 1u) / kMxStep, tile = (uint32_t)(t / steps), step = (uint32_t)(t % steps);
-    const uint32_t lane = threadIdx.x & 63u, row = tile * 16u + (lane & 15u);
-    const int32_t from = (int32_t)(step * kMxStep + (lane >> 4) * kMxBlock);
-    if (row >= s.rows) return;
-    float x[32];
-    load_row<T, N>(static_cast<const T *>(s.x) + (int64_t)row * s.stride, from, (int32_t)s.cols, x);
-    uint32_t scale;
-    const codes4 c = quantised(x, scale);
-    if (s.by_rows.codes) put(s.by_rows, tile, step, lane, c, scale);
-    if constexpr (VALUES) {
-        values_of<T>(c, scale, x);
-        store_row<T, N>(static_cast<T *>(s.values) + (int64_t)row * s.values_stride, from, (int32_t)s.cols, x);
+    constexpr uint32_t kAtOnce = kBlock / kRowLanes<T>, kTurns = 16u / kAtOnce;
+    const uint64_t at = first + blockIdx.x;
+    const uint32_t step = (uint32_t)(at % steps), base = (uint32_t)(at / steps) * 64u;
+    const uint32_t lane = threadIdx.x % kRowLanes<T>, sub = threadIdx.x / kRowLanes<T>, col = step * kMxStep + lane * kHas<T>;
+    const T *x = static_cast<const T *>(s.x);
+    const bool full = step * kMxStep + kMxStep <= s.cols;                // (of columns)
+    codes4 w[kTurns][4];
+#pragma unroll
+    for (uint32_t t = 0; t < kTurns; ++t)
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q) {
+            const uint32_t row = base + q * 16u + t * kAtOnce + sub;
+            w[t][q] = codes4{0u, 0u, 0u, 0u};
+            if (row < s.rows) w[t][q] = load_raw(x + (int64_t)row * s.stride, col, s.cols, full);
+        }
+#pragma unroll
+    for (uint32_t t = 0; t < kTurns; ++t) {
+        const uint32_t row0 = base + t * kAtOnce + sub;
+        uint32_t scales = 0, scale;
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q) {
+            const uint32_t row = row0 + q * 16u, c = row_codes<T>(w[t][q], scale);
+            scales |= scale << (8u * q);
+            if (row >= s.rows) continue;
+            if (s.by_rows.codes) put_codes<T>(s.by_rows, row, step, lane, c);
+            if constexpr (VALUES) store_raw(static_cast<T *>(s.values) + (int64_t)row * s.values_stride, col, s.cols, values_of<T>(c, scale));
+        }
+        if (s.by_rows.codes && lane % kBlockLanes<T> == 0 && row0 < s.rows) {
+            const global_ptr<uint8_t> to = in_global(s.by_rows.scales) + scales_at(s.by_rows, row0, step, lane / kBlockLanes<T>);
+            if (row0 + 48u < s.rows) *(global_ptr<uint32_t>)to = scales;
+            else for (uint32_t q = 0; q < 4; ++q) if (row0 + q * 16u < s.rows) to[q] = (uint8_t)(scales >> (8u * q));
+        }
     }
 }
 
-// Along the columns too: a block has 128 rows by 128 columns in LDS, of which it takes tiles of either direction.
+// ---- along the columns, and along the rows with them -----------------------------------------------------------------------
+// A wavefront has 128 columns of four (of 32-bit values: two) sets of 32 rows; a lane eight (four) columns of one set, in 128 registers.
 template <class T, bool ROWS, bool VALUES>
-__global__ __launch_bounds__(kBlock) void mx_cols_k(MxSource s, uint64_t first)
+__global__ __launch_bounds__(kBlock, 2) void mx_cols_k(MxSource s, uint64_t first, uint64_t tiles, uint32_t across)
 {
-    constexpr int N = 16 / (int)sizeof(T);
-    constexpr uint32_t kSide = 128, kPitch = kSide + 16 / sizeof(T);
-    __shared__ T held[kSide * kPitch];
-    const uint32_t across = (s.cols + kSide - 1u) / kSide;
-    const uint32_t br = (uint32_t)((first + blockIdx.x) / across), bc = (uint32_t)((first + blockIdx.x) % across), r0 = br * kSide, c0 = bc * kSide;
-    {
-        constexpr uint32_t wide = kSide / N;
-        for (uint32_t i = threadIdx.x; i < kSide * wide; i += kBlock) {
-            const uint32_t r = i / wide, c = i % wide * N;
-            float y[N];
-            if (r0 + r < s.rows) load_some<N, T, false>(in_global(static_cast<const T *>(s.x) + (int64_t)(r0 + r) * s.stride), (int32_t)(c0 + c), 0, (int32_t)s.cols, y);
-            else for (int e = 0; e < N; ++e) y[e] = 0.0f;
+    constexpr uint32_t kSets = 64u / kRowLanes<T>, kHigh = kSets * 32u;          // rows of a wavefront
+    const uint64_t at = (first + blockIdx.x) * (kBlock / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (at >= tiles) return;
+    const uint32_t step = (uint32_t)(at % across), lane = threadIdx.x & 63u, in_row = lane % kRowLanes<T>;
+    const uint32_t top = (uint32_t)(at / across) * kHigh, row0 = top + lane / kRowLanes<T> * 32u, col = step * kMxStep + in_row * kHas<T>;
+    const T *x = static_cast<const T *>(s.x);
+    codes4 w[32];
+    if (top + kHigh <= s.rows && step * kMxStep + kMxStep <= s.cols) {
+        const T *p = x + (int64_t)row0 * s.stride;
 #pragma unroll
-            for (int e = 0; e < N; ++e) held[r * kPitch + c + e] = (T)y[e];
+        for (uint32_t i = 0; i < 32; ++i) w[i] = load_raw(p + (int64_t)i * s.stride, col, s.cols, true);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 32; ++i) {
+            w[i] = codes4{0u, 0u, 0u, 0u};
+            if (row0 + i < s.rows) w[i] = load_raw(x + (int64_t)(row0 + i) * s.stride, col, s.cols, false);
         }
     }
-    __syncthreads();
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, in16 = lane & 15u, group = lane >> 4;
-    for (uint32_t k = wave; k < kSide / 16u; k += kBlock / 64u) {
-        float x[32];
-        uint32_t scale;
-        if constexpr (ROWS || VALUES) {
-            const uint32_t r = k * 16u + in16;
-            if (r0 + r < s.rows) {
+    // ---- columns: row0 is a multiple of 32 and the rows are the transposed matrix's columns
+    const uint32_t group = row0 % kMxStep / 32u;
+    const MxView &m = s.by_cols;
 #pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] = (float)held[r * kPitch + group * 32u + e];
-                const codes4 c = quantised(x, scale);
-                if constexpr (ROWS) put(s.by_rows, br * 8u + k, bc, lane, c, scale);
-                if constexpr (VALUES) {
-                    values_of<T>(c, scale, x);
-                    store_row<T, N>(static_cast<T *>(s.values) + (int64_t)(r0 + r) * s.values_stride, (int32_t)(c0 + group * 32u), (int32_t)s.cols, x);
+    for (uint32_t k = 0; k < 4; ++k) {
+        uint32_t most = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < 32; ++i) most = larger<T>(most, w[i][k]);
+#pragma unroll
+        for (uint32_t h = 0; h < kHas<T> / 4u; ++h) {                    // a word has one column, or two
+            const uint32_t c = col + k * (kHas<T> / 4u) + h;
+            const uint32_t scale = scale_of(bits_of<T>(sizeof(T) == 2 ? (h ? most >> 16 : most & 0xffffu) : most));
+            const float p = power_of(scale);
+            codes4 codes = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (uint32_t i = 0; i < 32; i += 8) {
+                uint32_t o = 0;
+                if constexpr (sizeof(T) == 2) {
+                    const uint32_t pick = h ? 0x07060302u : 0x05040100u;                     // the same half of two words
+                    o = pair_codes<T, 0>(o, __builtin_amdgcn_perm(w[i + 1][k], w[i][k], pick), p);
+                    o = pair_codes<T, 1>(o, __builtin_amdgcn_perm(w[i + 3][k], w[i + 2][k], pick), p);
+                    o = pair_codes<T, 2>(o, __builtin_amdgcn_perm(w[i + 5][k], w[i + 4][k], pick), p);
+                    o = pair_codes<T, 3>(o, __builtin_amdgcn_perm(w[i + 7][k], w[i + 6][k], pick), p);
+                } else {
+#define MC_PAIR(n) o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, float_of(w[i + 2 * n][k]), float_of(w[i + 2 * n + 1][k]), p, n)
+                    MC_PAIR(0); MC_PAIR(1); MC_PAIR(2); MC_PAIR(3);
+#undef MC_PAIR
                 }
+                codes[i / 8] = scale == 255u ? 0u : o;
+            }
+            if (c < s.cols) {
+                *(global_ptr<codes4>)(in_global(m.codes) + codes_at(m, c, row0 / kMxStep, group)) = codes;
+                in_global(m.scales)[scales_at(m, c, row0 / kMxStep, group) + c / 16u % 4u] = (uint8_t)scale;
             }
         }
-        const uint32_t col = k * 16u + in16;
-        if (c0 + col < s.cols) {
+    }
+    if constexpr (ROWS || VALUES) {
+        // 32 rows are two tiles of 16, and of one tile's 64 rows of scales
+        const uint32_t block = in_row / kBlockLanes<T>;
+        global_ptr<uint8_t> codes = {}, scales = {};
+        if constexpr (ROWS) {
+            codes = in_global(s.by_rows.codes) + codes_at(s.by_rows, row0, step, block) + in_row % kBlockLanes<T> * (16u / kBlockLanes<T>);
+            scales = in_global(s.by_rows.scales) + scales_at(s.by_rows, row0, step, block) + row0 / 16u % 4u;
+        }
 #pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = (float)held[(group * 32u + e) * kPitch + col];
-            const codes4 c = quantised(x, scale);
-            put(s.by_cols, bc * 8u + k, br, lane, c, scale);
+        for (uint32_t i = 0; i < 32; ++i) {
+            asm volatile("" : "+v"(w[i]));               // (or the magnitudes that the columns took from it are kept, in as many registers again)
+            uint32_t scale;
+            const uint32_t c = row_codes<T>(w[i], scale);
+            if (row0 + i >= s.rows) continue;
+            if constexpr (ROWS) {
+                const global_ptr<uint8_t> to = codes + (i / 16u ? (size_t)s.by_rows.steps * kMxCodes : 0u) + i % 16u * 16u;
+                if constexpr (sizeof(T) == 2) *(global_ptr<uint32_t>)to = c;
+                else *(global_ptr<uint16_t>)to = (uint16_t)c;
+                if (in_row % kBlockLanes<T> == 0) scales[i % 16u * 4u + i / 16u] = (uint8_t)scale;
+            }
+            if constexpr (VALUES) store_raw(static_cast<T *>(s.values) + (int64_t)(row0 + i) * s.values_stride, col, s.cols, values_of<T>(c, scale));
         }
     }
 }
@@ -166,13 +297,13 @@ static void quantize_of(const LaunchCtx &lc, const MxSource &s)
 {
     const uint32_t steps = (s.cols + kMxStep - 1u) / kMxStep;
     if (s.by_cols.codes) {
-        const uint64_t blocks = (uint64_t)((s.rows + 127u) / 128u) * ((s.cols + 127u) / 128u);
+        // (whole steps of 128 rows: the padding along the transposed matrix's rows is written too)
+        const uint64_t tiles = (uint64_t)((s.rows + kMxStep - 1u) / kMxStep) * (kMxStep / (64u / kRowLanes<T> * 32u)) * steps;
         auto k = s.by_rows.codes ? (s.values ? mx_cols_k<T, true, true> : mx_cols_k<T, true, false>) : s.values ? mx_cols_k<T, false, true> : mx_cols_k<T, false, false>;
-        in_launches(blocks, [&](uint64_t first, uint32_t n) { launch(k, dim3(n), dim3(kBlock), lc.stream, s, first); });
+        in_launches((tiles + kBlock / 64 - 1) / (kBlock / 64), [&](uint64_t first, uint32_t n) { launch(k, dim3(n), dim3(kBlock), lc.stream, s, first, tiles, steps); });
     } else {
-        const uint64_t tiles = (uint64_t)((s.rows + 15u) / 16u) * steps, blocks = (tiles + kBlock / 64 - 1) / (kBlock / 64);
         auto k = s.values ? mx_rows_k<T, true> : mx_rows_k<T, false>;
-        in_launches(blocks, [&](uint64_t first, uint32_t n) { launch(k, dim3(n), dim3(kBlock), lc.stream, s, first, tiles); });
+        in_launches((uint64_t)((s.rows + 63u) / 64u) * steps, [&](uint64_t first, uint32_t n) { launch(k, dim3(n), dim3(kBlock), lc.stream, s, first, steps); });
     }
 }
 void launch_mx_quantize(const LaunchCtx &lc, int dtype, const MxSource &s)
