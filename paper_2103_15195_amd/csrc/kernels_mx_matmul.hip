@@ -116,15 +116,15 @@ __device__ __forceinline__ v16f mma32(v4i x, v4i y, v16f acc, int sx, int sy)
     const v8i X = {x[0], x[1], x[2], x[3], 0, 0, 0, 0}, Y = {y[0], y[1], y[2], y[3], 0, 0, 0, 0};
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(X, Y, acc, 4, 4, QX, sx, QY, sy);
 }
-// A wavefront's operands for half a step: of either matrix PAIRS pairs of tiles, and a word of scales for two pairs (the first's in byte 0, the second's in byte 2).
-template <int PAIRS> struct Operands {
-    v4i a[PAIRS], b[PAIRS];
-    int sa[PAIRS / 2], sb[PAIRS / 2];
+// A wavefront's operands for half a step: PA and PB pairs of tiles, and a word of scales for two pairs (the first's in byte 0, the second's in byte 2).
+template <int PA, int PB> struct Operands {
+    v4i a[PA], b[PB];
+    int sa[PA / 2], sb[PB / 2];
 };
-// Products in groups of four, and behind each one what `also` issues for its number: instructions leave a wavefront in order, and what stands in front of
-// the products in a row keeps the matrix unit waiting.
-template <int PAIRS, class Also>
-__device__ __forceinline__ void multiply(const Operands<PAIRS> &o, v16f (&acc)[PAIRS][PAIRS], Also also)
+// Products, and behind each one what `also` issues for its number: instructions leave a wavefront in order, and what stands in front of the
+// products in a row keeps the matrix unit waiting.
+template <int PA, int PB, class Also>
+__device__ __forceinline__ void multiply(const Operands<PA, PB> &o, v16f (&acc)[PA][PB], Also also)
 {
     uint32_t i = 0;
 #define MC_ONE(dq, dr)                                                                                                        \
@@ -132,20 +132,30 @@ __device__ __forceinline__ void multiply(const Operands<PAIRS> &o, v16f (&acc)[P
     also(i++);                                                                                                                \
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int q = 0; q < PAIRS; q += 2)
+    for (int q = 0; q < PA; q += 2)
 #pragma unroll
-        for (int r = 0; r < PAIRS; r += 2) {
+        for (int r = 0; r < PB; r += 2) {
             MC_ONE(0, 0) MC_ONE(0, 1) MC_ONE(1, 0) MC_ONE(1, 1)
         }
 #undef MC_ONE
 }
-
-template <class T, int PAIRS>
-__global__ __launch_bounds__(kBlock, PAIRS == 4 ? 1 : 2) void mx_matmul_lds_k(MxProduct p, uint32_t tiles_a, uint32_t tiles_b)
+// N sums of a row, to memory as T.
+template <class T, int N>
+__device__ __forceinline__ void store_sums(global_ptr<T> to, const float (&x)[N])
 {
-    constexpr uint32_t kTiles = 4 * PAIRS, kStages = 4;             // tiles of 16 rows to a block
-    constexpr uint32_t kCodesA = 0, kCodesB = kTiles * kMxCodes, kScalesA = 2 * kCodesB, kScalesB = kScalesA + kTiles / 4 * kMxScales,
-                       kStage = kScalesB + kTiles / 4 * kMxScales;
+    typedef typename VecOf<T, N>::type vec;
+    vec v;
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = (T)x[e];
+    __builtin_nontemporal_store(v, (global_ptr<vec>)to);
+}
+
+template <class T, int PA, int PB, int STAGES, int BLOCKS>
+__global__ __launch_bounds__(kBlock, BLOCKS) void mx_matmul_lds_k(MxProduct p, uint32_t tiles_a, uint32_t tiles_b)
+{
+    constexpr uint32_t kTilesA = 4 * PA, kTilesB = 4 * PB, kStages = STAGES;             // tiles of 16 rows to a block
+    constexpr uint32_t kCodesA = 0, kCodesB = kTilesA * kMxCodes, kScalesA = kCodesB + kTilesB * kMxCodes, kScalesB = kScalesA + kTilesA / 4 * kMxScales,
+                       kStage = kScalesB + kTilesB / 4 * kMxScales;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * kStage];
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u;
     // Blocks go to the eight dies in turn: each die gets a run of tiles, eight rows of them by as many columns as that takes.
@@ -159,27 +169,31 @@ __global__ __launch_bounds__(kBlock, PAIRS == 4 ? 1 : 2) void mx_matmul_lds_k(Mx
         tj = in / high;
     }
     const uint32_t steps = p.a.steps;
-    const uint64_t first_a = (uint64_t)ti * kTiles, first_b = (uint64_t)tj * kTiles;                // tiles of 16
+    const uint64_t first_a = (uint64_t)ti * kTilesA, first_b = (uint64_t)tj * kTilesB;                // tiles of 16
     const uint64_t line = (uint64_t)steps * kMxCodes, line_s = (uint64_t)steps * kMxScales;
     const rsrc_t codes_a = buffer_at(p.a.codes + first_a * line, ((p.a.rows + 15u) / 16u - first_a) * line);
     const rsrc_t codes_b = buffer_at(p.b.codes + first_b * line, ((p.b.rows + 15u) / 16u - first_b) * line);
     const rsrc_t scales_a = buffer_at(p.a.scales + first_a / 4u * line_s, ((p.a.rows + 63u) / 64u - first_a / 4u) * line_s);
     const rsrc_t scales_b = buffer_at(p.b.scales + first_b / 4u * line_s, ((p.b.rows + 63u) / 64u - first_b / 4u) * line_s);
     const uint32_t lane16 = lane * 16u, lane4 = lane * 4u, at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
-    // A wavefront copies a quarter of the step's tiles of either operand, and of the scales (PAIRS == 2: each wavefront one tile of the four).
-    constexpr uint32_t kMine = kTiles / 4, kCopies = 2 * kMine + kTiles / 8;
+    // A wavefront copies a quarter of the step's tiles of either operand, a tile of a's scales and one of b's.
+    static_assert(PA == 4 && PB <= 4, "a tile of scales to a wavefront");
+    constexpr uint32_t kMineA = kTilesA / 4, kMineB = kTilesB / 4, kCopies = kMineA + kMineB + 2;
     // the k-th of a wavefront's copies for step s
     const auto copy = [&](uint32_t s, uint32_t k) {
         const uint32_t to = at + s % kStages * kStage;
-        if (k < 2u * kMine) {
-            const uint32_t t = wave * kMine + k / 2u;
-            if (k % 2u == 0) copy16(to + kCodesA + t * kMxCodes, codes_a, (t * steps + s) * kMxCodes + lane16);
-            else copy16(to + kCodesB + t * kMxCodes, codes_b, (t * steps + s) * kMxCodes + lane16);
-        } else if constexpr (PAIRS == 4) {
-            if (k % 2u == 0) copy4(to + kScalesA + wave * kMxScales, scales_a, (wave * steps + s) * kMxScales + lane4);
-            else copy4(to + kScalesB + wave * kMxScales, scales_b, (wave * steps + s) * kMxScales + lane4);
-        } else if (wave < 2u) copy4(to + kScalesA + wave * kMxScales, scales_a, (wave * steps + s) * kMxScales + lane4);
-        else copy4(to + kScalesB + (wave - 2u) * kMxScales, scales_b, ((wave - 2u) * steps + s) * kMxScales + lane4);
+        if (k < kMineA) {
+            const uint32_t t = wave * kMineA + k;
+            copy16(to + kCodesA + t * kMxCodes, codes_a, (t * steps + s) * kMxCodes + lane16);
+        } else if (k < kMineA + kMineB) {
+            const uint32_t t = wave * kMineB + k - kMineA;
+            copy16(to + kCodesB + t * kMxCodes, codes_b, (t * steps + s) * kMxCodes + lane16);
+        } else if (k == kMineA + kMineB) {
+            copy4(to + kScalesA + wave * kMxScales, scales_a, (wave * steps + s) * kMxScales + lane4);
+        } else {                         // (of two tiles the second is copied three times: the same bytes, and the same number of copies in each wavefront)
+            const uint32_t t = wave < PB ? wave : PB - 1u;
+            copy4(to + kScalesB + t * kMxScales, scales_b, (t * steps + s) * kMxScales + lane4);
+        }
     };
     const auto copies = [&](uint32_t s, uint32_t from, uint32_t n) {
 #pragma unroll
@@ -189,66 +203,96 @@ __global__ __launch_bounds__(kBlock, PAIRS == 4 ? 1 : 2) void mx_matmul_lds_k(Mx
     const uint32_t other = lane >> 4 & 1u;                               // which tile of a pair the lane's row is of
     const uint32_t mine16 = other * kMxCodes + (lane >> 5) * 256u + (lane & 15u) * 16u, mine4 = (lane >> 5) * 64u + (lane & 15u) * 4u;
     // the k-th read of half a step's operands
-    constexpr uint32_t kReads = 3 * PAIRS;
-    const auto read = [&](uint32_t s, uint32_t half, Operands<PAIRS> &o, uint32_t k) {
+    constexpr uint32_t kReads = PA / 2 + PB / 2 + PA + PB;
+    const auto read = [&](uint32_t s, uint32_t half, Operands<PA, PB> &o, uint32_t k) {
         const uint8_t *from = lds + s % kStages * kStage;
-        if (k < PAIRS) {
-            const uint32_t q = k / 2u;
-            if (k % 2u == 0) o.sa[q] = *reinterpret_cast<const int *>(from + kScalesA + (half_a * (PAIRS / 2) + q) * kMxScales + half * 128u + mine4) >> (8u * other);
-            else o.sb[q] = *reinterpret_cast<const int *>(from + kScalesB + (half_b * (PAIRS / 2) + q) * kMxScales + half * 128u + mine4) >> (8u * other);
+        if (k < PA / 2) {
+            o.sa[k] = *reinterpret_cast<const int *>(from + kScalesA + (half_a * (PA / 2) + k) * kMxScales + half * 128u + mine4) >> (8u * other);
+        } else if (k < PA / 2 + PB / 2) {
+            const uint32_t q = k - PA / 2;
+            o.sb[q] = *reinterpret_cast<const int *>(from + kScalesB + (half_b * (PB / 2) + q) * kMxScales + half * 128u + mine4) >> (8u * other);
+        } else if (k < PA / 2 + PB / 2 + PB) {
+            const uint32_t q = k - PA / 2 - PB / 2;
+            o.b[q] = *reinterpret_cast<const v4i *>(from + kCodesB + (half_b * PB + q) * 2u * kMxCodes + half * 512u + mine16);
         } else {
-            const uint32_t q = (k - PAIRS) / 2u;
-            if (k % 2u == 0) o.b[q] = *reinterpret_cast<const v4i *>(from + kCodesB + (half_b * PAIRS + q) * 2u * kMxCodes + half * 512u + mine16);
-            else o.a[q] = *reinterpret_cast<const v4i *>(from + kCodesA + (half_a * PAIRS + q) * 2u * kMxCodes + half * 512u + mine16);
+            const uint32_t q = k - PA / 2 - PB / 2 - PB;
+            o.a[q] = *reinterpret_cast<const v4i *>(from + kCodesA + (half_a * PA + q) * 2u * kMxCodes + half * 512u + mine16);
         }
     };
-    v16f acc[PAIRS][PAIRS] = {};
-    Operands<PAIRS> first, second;
+    v16f acc[PA][PB] = {};
+    Operands<PA, PB> first, second;
     // (Steps behind the last are copied too, from the next rows or as zeros, so that the number of copies under way is always the same; nothing multiplies them.)
-    constexpr uint32_t kEarly = kCopies / 2, kProducts = PAIRS * PAIRS;
+    // With four stages a step's copies are issued half before and half behind a barrier, with three all behind it.
+    constexpr uint32_t kAhead = kStages - 1, kEarly = kStages == 4 ? kCopies / 2 : kCopies, kProducts = PA * PB;
     copies(0, 0, kCopies);
-    copies(1, 0, kCopies);
-    copied<kCopies>();
-    copies(2, 0, kEarly);
+    copies(1, 0, kStages == 4 ? kCopies : 0);
+    copied<kStages == 4 ? kCopies : 0>();
+    copies(kAhead - 1, 0, kEarly);
 #pragma unroll
     for (uint32_t k = 0; k < kReads; ++k) read(0, 0, first, k);
     for (uint32_t s = 0; s < steps; ++s) {
-        multiply<PAIRS>(first, acc, [&](uint32_t i) {
+        multiply<PA, PB>(first, acc, [&](uint32_t i) {
 #pragma unroll
             for (uint32_t k = i * kReads / kProducts; k < (i + 1) * kReads / kProducts; ++k) read(s, 1, second, k);
 #pragma unroll
-            for (uint32_t k = i * (kCopies - kEarly) / kProducts; k < (i + 1) * (kCopies - kEarly) / kProducts; ++k) copy(s + 2, kEarly + k);
+            for (uint32_t k = i * (kCopies - kEarly) / kProducts; k < (i + 1) * (kCopies - kEarly) / kProducts; ++k) copy(s + kAhead - 1, kEarly + k);
         });
-        // step s + 1 is there, and every wavefront has read step s - 1, whose place step s + 3 takes
-        copied<kCopies>();
-        multiply<PAIRS>(second, acc, [&](uint32_t i) {
+        // step s + 1 is there, and every wavefront has read step s - 1, whose place the next copies take
+        copied<kStages == 4 ? kCopies : 0>();
+        multiply<PA, PB>(second, acc, [&](uint32_t i) {
 #pragma unroll
             for (uint32_t k = i * kReads / kProducts; k < (i + 1) * kReads / kProducts; ++k) read(s + 1, 0, first, k);
 #pragma unroll
-            for (uint32_t k = i * kEarly / kProducts; k < (i + 1) * kEarly / kProducts; ++k) copy(s + 3, k);
+            for (uint32_t k = i * kEarly / kProducts; k < (i + 1) * kEarly / kProducts; ++k) copy(s + kAhead, k);
         });
     }
     copied<0>();                         // (no copy outlives the block, and no wavefront reads operands any more)
-    // Results by rows: each wavefront turns its 32 x 32 PAIRS of them round in a part of LDS of its own, so that what a wavefront stores are whole lines.
-    constexpr uint32_t kWide = 32 * PAIRS, kPitch = kWide + 4;           // floats to a row
+    // Results by rows: each wavefront turns its sets of 32 rows round in a part of LDS of its own, so that what a wavefront stores are whole lines.
+    constexpr uint32_t kWide = 32 * PB, kPitch = kWide + 4;              // floats to a row
     static_assert(4 * 32 * kPitch * sizeof(float) <= sizeof(lds), "a part of LDS for each wavefront");
     float *const own = reinterpret_cast<float *>(lds) + wave * 32u * kPitch;
-    const uint32_t row0 = ((uint32_t)first_a + half_a * PAIRS * 2u) * 16u, col0 = ((uint32_t)first_b + half_b * PAIRS * 2u) * 16u;
+    const uint32_t row0 = ((uint32_t)first_a + half_a * PA * 2u) * 16u, col0 = ((uint32_t)first_b + half_b * PB * 2u) * 16u;
+    constexpr int N = 16 / (int)sizeof(T);                               // columns of a lane
+    constexpr uint32_t kLanes = kWide / N, kRows = 64u / kLanes;
+    const uint32_t mine = lane % kLanes * N;
+    const bool whole = col0 + kWide <= p.b.rows;
+    float bias[N];
 #pragma unroll
-    for (uint32_t q = 0; q < PAIRS; ++q) {
+    for (int e = 0; e < N; ++e) bias[e] = 0.0f;
+    if (p.bias && whole) {
 #pragma unroll
-        for (uint32_t r = 0; r < PAIRS; ++r)
+        for (int e = 0; e < N; ++e) bias[e] = in_global(p.bias)[col0 + mine + e];
+    }
+#pragma unroll
+    for (uint32_t q = 0; q < PA; ++q) {
+#pragma unroll
+        for (uint32_t r = 0; r < PB; ++r)
 #pragma unroll
             for (uint32_t n = 0; n < 4; ++n)
                 *reinterpret_cast<v4f *>(own + (lane & 31u) * kPitch + r * 32u + n * 8u + (lane >> 5) * 4u) =
                     v4f{acc[q][r][4 * n], acc[q][r][4 * n + 1], acc[q][r][4 * n + 2], acc[q][r][4 * n + 3]};
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        constexpr uint32_t kLanes = kWide / 4u, kRows = 64u / kLanes;    // four columns a lane
-#pragma unroll 4
-        for (uint32_t i = 0; i < 32u; i += kRows) {
-            const uint32_t r = i + lane / kLanes, c = lane % kLanes * 4u;
-            finish<T>(p, row0 + q * 32u + r, col0 + c, *reinterpret_cast<const v4f *>(own + r * kPitch + c));
+        const uint32_t top = row0 + q * 32u;
+        if (whole && top + 32u <= p.a.rows && !p.accumulate) {
+            global_ptr<T> to = in_global(static_cast<T *>(p.out)) + (int64_t)(top + lane / kLanes) * p.stride + col0 + mine;
+#pragma unroll
+            for (uint32_t i = 0; i < 32u; i += kRows, to += kRows * p.stride) {
+                float x[N];
+#pragma unroll
+                for (int e = 0; e < N; e += 4) {
+                    const v4f y = *reinterpret_cast<const v4f *>(own + (i + lane / kLanes) * kPitch + mine + e);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[e + k] = y[k] + bias[e + k];
+                }
+                store_sums<T, N>(to, x);
+            }
+        } else {
+#pragma unroll 1
+            for (uint32_t i = 0; i < 32u; i += kRows)
+#pragma unroll 1
+                for (uint32_t e = 0; e < N; e += 4)
+                    finish<T>(p, top + i + lane / kLanes, col0 + mine + e, *reinterpret_cast<const v4f *>(own + (i + lane / kLanes) * kPitch + mine + e));
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -261,7 +305,8 @@ static void matmul_of(const LaunchCtx &lc, const MxProduct &p)
     if (p.a.rows > 128u && p.a.steps < (1u << 16)) {
         const uint32_t ta = (p.a.rows + 255u) / 256u, tb = (p.b.rows + 255u) / 256u;
         if ((uint64_t)ta * tb < (1u << 23)) {
-            launch(mx_matmul_lds_k<T, 4>, dim3(ta * tb), dim3(kBlock), lc.stream, p, ta, tb);
+            if (getenv("T4")) { const uint32_t tb = (p.b.rows + 127u) / 128u; launch(mx_matmul_lds_k<T, 4, 2, 3, 2>, dim3(ta * tb), dim3(kBlock), lc.stream, p, ta, tb); }
+            else launch(mx_matmul_lds_k<T, 4, 4, 4, 1>, dim3(ta * tb), dim3(kBlock), lc.stream, p, ta, tb);
             return;
         }
     }
