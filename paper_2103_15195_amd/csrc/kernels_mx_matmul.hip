@@ -40,47 +40,81 @@ __device__ __forceinline__ void finish(const MxProduct &p, uint32_t i, uint32_t 
     store_some<4, T>(row, (int32_t)j, 0, hi, y);
 }
 
-// 128 x 128 outputs to a block of four wavefronts of 64 x 64, operands straight from memory.
-template <class T>
-__global__ __launch_bounds__(kBlock) void mx_matmul_k(MxProduct p, uint64_t first, uint32_t tiles_b)
+// ---- few rows -------------------------------------------------------------------------------------------------------------
+// Operands straight from memory, b's past the caches: a block of eight wavefronts has 16 MT rows by 16 NT columns of outputs, which its wavefronts sum over steps
+// of their own (the w-th over the w-th, w + 8-th ... step, so that they read b's tiles in one run), and SPLITS blocks share the steps where they are very many.
+constexpr uint32_t kFewWaves = 8;
+template <int MT, int NT> struct FewStep {   // operands of one step
+    v4i a[MT], b[NT];
+    int sa, sb;
+};
+template <int MT, int NT, int Q = 0, int R = 0>
+__device__ __forceinline__ void few_products(const FewStep<MT, NT> &o, v4f (&acc)[MT][NT])
 {
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u;
-    const uint32_t ti = (uint32_t)((first + blockIdx.x) / tiles_b) * 2u + wave / 2u, tj = (uint32_t)((first + blockIdx.x) % tiles_b) * 2u + wave % 2u;        // tiles of 64
-    if (ti * 64u >= p.a.rows || tj * 64u >= p.b.rows) return;
-    const uint32_t last_a = (p.a.rows - 1u) / 16u, last_b = (p.b.rows - 1u) / 16u, steps = p.a.steps;
-    global_ptr<const v4i> at[4], bt[4];
-#pragma unroll
-    for (uint32_t q = 0; q < 4; ++q) {           // (tiles beyond the last row stand for the last one: what they give is not stored)
-        const uint32_t ra = ti * 4u + q < last_a ? ti * 4u + q : last_a, rb = tj * 4u + q < last_b ? tj * 4u + q : last_b;
-        at[q] = (global_ptr<const v4i>)in_global(p.a.codes + (size_t)ra * steps * kMxCodes) + lane;
-        bt[q] = (global_ptr<const v4i>)in_global(p.b.codes + (size_t)rb * steps * kMxCodes) + lane;
+    if constexpr (Q < MT) {
+        acc[Q][R] = mma<R, Q>(o.b[R], o.a[Q], acc[Q][R], o.sb, o.sa);
+        few_products<MT, NT, R + 1 < NT ? Q : Q + 1, R + 1 < NT ? R + 1 : 0>(o, acc);
     }
-    const global_ptr<const int> as = (global_ptr<const int>)in_global(p.a.scales + (size_t)ti * steps * kMxScales) + lane;
-    const global_ptr<const int> bs = (global_ptr<const int>)in_global(p.b.scales + (size_t)tj * steps * kMxScales) + lane;
-    v4f acc[4][4] = {};
-    for (uint32_t s = 0; s < steps; ++s) {
-        v4i x[4], y[4];
+}
+template <class T, int MT, int NT>
+__global__ __launch_bounds__(kFewWaves * 64) void mx_matmul_few_k(MxProduct p, uint64_t first, uint32_t tiles_b, uint32_t splits)
+{
+    constexpr int kDeep = MT * NT <= 4 ? 4 : 2;      // steps on their way at once
+    __shared__ v4f sums[kFewWaves][MT * NT][64];
+    const uint32_t waves = blockDim.x / 64u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u;
+    const uint64_t at = (first + blockIdx.x) / splits;
+    const uint32_t split = (uint32_t)((first + blockIdx.x) % splits), ti = (uint32_t)(at / tiles_b), tj = (uint32_t)(at % tiles_b), steps = p.a.steps;
+    const uint32_t from = (uint32_t)((uint64_t)steps * split / splits), to = (uint32_t)((uint64_t)steps * (split + 1u) / splits);
+    const uint32_t last_a = (p.a.rows - 1u) / 16u, last_b = (p.b.rows - 1u) / 16u;
+    global_ptr<const v4i> ap[MT], bp[NT];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) { x[q] = at[q][s * 64u]; y[q] = bt[q][s * 64u]; }
-        const int sx = as[s * 64u], sy = bs[s * 64u];
-#define MC_ROW(q)                                              \
-        acc[q][0] = mma<0, q>(y[0], x[q], acc[q][0], sy, sx);  \
-        acc[q][1] = mma<1, q>(y[1], x[q], acc[q][1], sy, sx);  \
-        acc[q][2] = mma<2, q>(y[2], x[q], acc[q][2], sy, sx);  \
-        acc[q][3] = mma<3, q>(y[3], x[q], acc[q][3], sy, sx);
-        MC_ROW(0) MC_ROW(1) MC_ROW(2) MC_ROW(3)
-#undef MC_ROW
+    for (uint32_t q = 0; q < MT; ++q) {              // (tiles beyond the last row stand for the last one: what they give is not stored)
+        const uint32_t r = ti * MT + q < last_a ? ti * MT + q : last_a;
+        ap[q] = (global_ptr<const v4i>)in_global(p.a.codes + (size_t)r * steps * kMxCodes) + lane;
     }
 #pragma unroll
-    for (uint32_t q = 0; q < 4; ++q)
+    for (uint32_t q = 0; q < NT; ++q) {
+        const uint32_t r = tj * NT + q < last_b ? tj * NT + q : last_b;
+        bp[q] = (global_ptr<const v4i>)in_global(p.b.codes + (size_t)r * steps * kMxCodes) + lane;
+    }
+    const global_ptr<const int> as = (global_ptr<const int>)in_global(p.a.scales + (size_t)(ti * MT / 4u) * steps * kMxScales) + lane;
+    const global_ptr<const int> bs = (global_ptr<const int>)in_global(p.b.scales + (size_t)(tj * NT / 4u) * steps * kMxScales) + lane;
+    const uint32_t turn_a = ti * MT % 4u * 8u, turn_b = tj * NT % 4u * 8u;               // which bytes of a word of scales are the tiles'
+    v4f acc[MT][NT] = {};
+    for (uint32_t s = from + wave; s < to; s += kDeep * waves) {
+        FewStep<MT, NT> o[kDeep];
 #pragma unroll
-        for (uint32_t r = 0; r < 4; ++r)
-            finish<T>(p, ti * 64u + q * 16u + (lane & 15u), tj * 64u + r * 16u + (lane >> 4) * 4u, acc[q][r]);
+        for (int k = 0; k < kDeep; ++k) {
+            const uint32_t n = s + k * waves < to ? s + k * waves : to - 1u;             // (again, where there are no more)
+#pragma unroll
+            for (int q = 0; q < NT; ++q) o[k].b[q] = __builtin_nontemporal_load(bp[q] + n * 64u);
+            o[k].sb = bs[n * 64u] >> turn_b;
+#pragma unroll
+            for (int q = 0; q < MT; ++q) o[k].a[q] = ap[q][n * 64u];
+            o[k].sa = as[n * 64u] >> turn_a;
+        }
+#pragma unroll
+        for (int k = 0; k < kDeep; ++k) if (s + k * waves < to) few_products<MT, NT>(o[k], acc);
+    }
+#pragma unroll
+    for (int q = 0; q < MT; ++q)
+#pragma unroll
+        for (int r = 0; r < NT; ++r) sums[wave][q * NT + r][lane] = acc[q][r];
+    __syncthreads();
+    // Tile f of MT NT belongs to wavefront f % waves; sums are taken in the order of the wavefronts.
+    p.out = static_cast<T *>(p.out) + split * p.apart;
+    const uint32_t row = ti * 16u * MT + (lane & 15u), col = tj * 16u * NT + (lane >> 4) * 4u;
+    for (uint32_t f = wave; f < MT * NT; f += waves) {
+        v4f x = sums[0][f][lane];
+        for (uint32_t w = 1; w < waves; ++w) x += sums[w][f][lane];
+        finish<T>(p, row + f / NT * 16u, col + f % NT * 16u, x);
+    }
 }
 
 // ---- many rows -----------------------------------------------------------------------------------------------------------
-// Operands through LDS: a block of four wavefronts has SIDE x SIDE outputs, a wavefront a quarter of them.  A step's codes and scales are copied straight
-// to LDS, three steps ahead; a wavefront reads the next step's operands while it multiplies this one's.
+// Operands through LDS: four wavefronts have 64 PA x 64 PB outputs, each a quarter of them.  A step's codes and scales are copied straight to LDS, three steps
+// ahead; a wavefront reads the operands of the next half step while it multiplies this one's.  With GROUPS = 2 a block has two such fours, which take
+// half of the steps each.
 typedef uint32_t rsrc_t __attribute__((ext_vector_type(4)));
 // What a buffer's loads go by: beyond `bytes` they give 0.
 __device__ __forceinline__ rsrc_t buffer_at(const uint8_t *p, uint64_t bytes)
@@ -150,35 +184,41 @@ __device__ __forceinline__ void store_sums(global_ptr<T> to, const float (&x)[N]
     __builtin_nontemporal_store(v, (global_ptr<vec>)to);
 }
 
-template <class T, int PA, int PB, int STAGES, int BLOCKS>
-__global__ __launch_bounds__(kBlock, BLOCKS) void mx_matmul_lds_k(MxProduct p, uint32_t tiles_a, uint32_t tiles_b)
+template <class T, int PA, int PB, int GROUPS>
+__global__ __launch_bounds__(kBlock * GROUPS, GROUPS == 1 ? 1 : 2) void mx_matmul_lds_k(MxProduct p, uint32_t tiles_a, uint32_t tiles_b, uint32_t splits)
 {
-    constexpr uint32_t kTilesA = 4 * PA, kTilesB = 4 * PB, kStages = STAGES;             // tiles of 16 rows to a block
+    constexpr uint32_t kTilesA = 4 * PA, kTilesB = 4 * PB, kStages = 4;             // tiles of 16 rows to a block
     constexpr uint32_t kCodesA = 0, kCodesB = kTilesA * kMxCodes, kScalesA = kCodesB + kTilesB * kMxCodes, kScalesB = kScalesA + kTilesA / 4 * kMxScales,
                        kStage = kScalesB + kTilesB / 4 * kMxScales;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * kStage];
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63u;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[GROUPS * kStages * kStage];
+    const uint32_t group = __builtin_amdgcn_readfirstlane(threadIdx.x / kBlock), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % 4u, lane = threadIdx.x & 63u;
     // Blocks go to the eight dies in turn: each die gets a run of tiles, eight rows of them by as many columns as that takes.
-    uint32_t ti, tj;
+    uint32_t ti, tj, split;
     {
         constexpr uint32_t kDies = 8, kHigh = 8;
-        const uint32_t all = tiles_a * tiles_b, die = blockIdx.x % kDies, each = all / kDies, more = all % kDies;
-        const uint32_t t = die * each + (die < more ? die : more) + blockIdx.x / kDies;
+        const uint32_t all = tiles_a * tiles_b * splits, die = blockIdx.x % kDies, each = all / kDies, more = all % kDies;
+        const uint32_t n = die * each + (die < more ? die : more) + blockIdx.x / kDies, t = n / splits;
+        split = n % splits;
         const uint32_t band = t / (kHigh * tiles_b), in = t % (kHigh * tiles_b), high = tiles_a - band * kHigh < kHigh ? tiles_a - band * kHigh : kHigh;
         ti = band * kHigh + in % high;
         tj = in / high;
     }
-    const uint32_t steps = p.a.steps;
+    const uint32_t steps = p.a.steps, parts = splits * GROUPS, part = split * GROUPS + group;
+    const uint32_t begin = (uint32_t)((uint64_t)steps * part / parts), end = (uint32_t)((uint64_t)steps * (part + 1u) / parts);
+    const uint32_t turns = (steps + parts - 1u) / parts;                 // the most steps that a part has
     const uint64_t first_a = (uint64_t)ti * kTilesA, first_b = (uint64_t)tj * kTilesB;                // tiles of 16
     const uint64_t line = (uint64_t)steps * kMxCodes, line_s = (uint64_t)steps * kMxScales;
     const rsrc_t codes_a = buffer_at(p.a.codes + first_a * line, ((p.a.rows + 15u) / 16u - first_a) * line);
     const rsrc_t codes_b = buffer_at(p.b.codes + first_b * line, ((p.b.rows + 15u) / 16u - first_b) * line);
     const rsrc_t scales_a = buffer_at(p.a.scales + first_a / 4u * line_s, ((p.a.rows + 63u) / 64u - first_a / 4u) * line_s);
     const rsrc_t scales_b = buffer_at(p.b.scales + first_b / 4u * line_s, ((p.b.rows + 63u) / 64u - first_b / 4u) * line_s);
-    const uint32_t lane16 = lane * 16u, lane4 = lane * 4u, at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
-    // A wavefront copies a quarter of the step's tiles of either operand, a tile of a's scales and one of b's.
-    static_assert(PA == 4 && PB <= 4, "a tile of scales to a wavefront");
-    constexpr uint32_t kMineA = kTilesA / 4, kMineB = kTilesB / 4, kCopies = kMineA + kMineB + 2;
+    const uint32_t lane16 = lane * 16u, lane4 = lane * 4u, at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds + group * (kStages * kStage);
+    // A wavefront copies a quarter of the step's tiles of either operand, and of the PA + PB tiles of scales one or two.
+    static_assert(PA == PB, "scales are handed out evenly");
+    constexpr uint32_t kMineA = kTilesA / 4, kMineB = kTilesB / 4, kCopies = kMineA + kMineB + PA / 2;
+    const bool of_b = PA == 2 && wave >= 2u;
+    const uint32_t tile_s = of_b ? wave - 2u : wave, scales_to = (of_b ? kScalesB : kScalesA) + tile_s * kMxScales;
+    const rsrc_t scales_1 = of_b ? scales_b : scales_a;
     // the k-th of a wavefront's copies for step s
     const auto copy = [&](uint32_t s, uint32_t k) {
         const uint32_t to = at + s % kStages * kStage;
@@ -188,12 +228,8 @@ __global__ __launch_bounds__(kBlock, BLOCKS) void mx_matmul_lds_k(MxProduct p, u
         } else if (k < kMineA + kMineB) {
             const uint32_t t = wave * kMineB + k - kMineA;
             copy16(to + kCodesB + t * kMxCodes, codes_b, (t * steps + s) * kMxCodes + lane16);
-        } else if (k == kMineA + kMineB) {
-            copy4(to + kScalesA + wave * kMxScales, scales_a, (wave * steps + s) * kMxScales + lane4);
-        } else {                         // (of two tiles the second is copied three times: the same bytes, and the same number of copies in each wavefront)
-            const uint32_t t = wave < PB ? wave : PB - 1u;
-            copy4(to + kScalesB + t * kMxScales, scales_b, (t * steps + s) * kMxScales + lane4);
-        }
+        } else if (k == kMineA + kMineB) copy4(to + scales_to, scales_1, (tile_s * steps + s) * kMxScales + lane4);
+        else copy4(to + kScalesB + wave * kMxScales, scales_b, (wave * steps + s) * kMxScales + lane4);
     };
     const auto copies = [&](uint32_t s, uint32_t from, uint32_t n) {
 #pragma unroll
@@ -205,7 +241,7 @@ __global__ __launch_bounds__(kBlock, BLOCKS) void mx_matmul_lds_k(MxProduct p, u
     // the k-th read of half a step's operands
     constexpr uint32_t kReads = PA / 2 + PB / 2 + PA + PB;
     const auto read = [&](uint32_t s, uint32_t half, Operands<PA, PB> &o, uint32_t k) {
-        const uint8_t *from = lds + s % kStages * kStage;
+        const uint8_t *from = lds + group * (kStages * kStage) + s % kStages * kStage;
         if (k < PA / 2) {
             o.sa[k] = *reinterpret_cast<const int *>(from + kScalesA + (half_a * (PA / 2) + k) * kMxScales + half * 128u + mine4) >> (8u * other);
         } else if (k < PA / 2 + PB / 2) {
@@ -222,36 +258,59 @@ __global__ __launch_bounds__(kBlock, BLOCKS) void mx_matmul_lds_k(MxProduct p, u
     v16f acc[PA][PB] = {};
     Operands<PA, PB> first, second;
     // (Steps behind the last are copied too, from the next rows or as zeros, so that the number of copies under way is always the same; nothing multiplies them.)
-    // With four stages a step's copies are issued half before and half behind a barrier, with three all behind it.
-    constexpr uint32_t kAhead = kStages - 1, kEarly = kStages == 4 ? kCopies / 2 : kCopies, kProducts = PA * PB;
-    copies(0, 0, kCopies);
-    copies(1, 0, kStages == 4 ? kCopies : 0);
-    copied<kStages == 4 ? kCopies : 0>();
-    copies(kAhead - 1, 0, kEarly);
+    // A step's copies are issued half behind one barrier and half before the next.
+    constexpr uint32_t kEarly = kCopies / 2, kProducts = PA * PB;
+    copies(begin, 0, kCopies);
+    copies(begin + 1, 0, kCopies);
+    copied<kCopies>();
+    copies(begin + 2, 0, kEarly);
 #pragma unroll
-    for (uint32_t k = 0; k < kReads; ++k) read(0, 0, first, k);
-    for (uint32_t s = 0; s < steps; ++s) {
-        multiply<PA, PB>(first, acc, [&](uint32_t i) {
+    for (uint32_t k = 0; k < kReads; ++k) read(begin, 0, first, k);
+    for (uint32_t s = begin; s < begin + turns; ++s) {
+        const bool any = GROUPS == 1 || s < end;                         // (a group may have a step less than the other: it only waits)
+        if (any) multiply<PA, PB>(first, acc, [&](uint32_t i) {
 #pragma unroll
             for (uint32_t k = i * kReads / kProducts; k < (i + 1) * kReads / kProducts; ++k) read(s, 1, second, k);
 #pragma unroll
-            for (uint32_t k = i * (kCopies - kEarly) / kProducts; k < (i + 1) * (kCopies - kEarly) / kProducts; ++k) copy(s + kAhead - 1, kEarly + k);
+            for (uint32_t k = i * (kCopies - kEarly) / kProducts; k < (i + 1) * (kCopies - kEarly) / kProducts; ++k) copy(s + 2, kEarly + k);
         });
         // step s + 1 is there, and every wavefront has read step s - 1, whose place the next copies take
-        copied<kStages == 4 ? kCopies : 0>();
-        multiply<PA, PB>(second, acc, [&](uint32_t i) {
+        copied<kCopies>();
+        if (any) multiply<PA, PB>(second, acc, [&](uint32_t i) {
 #pragma unroll
             for (uint32_t k = i * kReads / kProducts; k < (i + 1) * kReads / kProducts; ++k) read(s + 1, 0, first, k);
 #pragma unroll
-            for (uint32_t k = i * kEarly / kProducts; k < (i + 1) * kEarly / kProducts; ++k) copy(s + kAhead, k);
+            for (uint32_t k = i * kEarly / kProducts; k < (i + 1) * kEarly / kProducts; ++k) copy(s + 3, k);
         });
     }
     copied<0>();                         // (no copy outlives the block, and no wavefront reads operands any more)
+    constexpr uint32_t kKept = PA / GROUPS;                              // sets of 32 rows that a group finishes
+    const uint32_t kept = group * kKept;
+    v16f (&sum)[kKept][PB] = reinterpret_cast<v16f (&)[kKept][PB]>(acc);
+    if constexpr (GROUPS == 2) {         // each group gives the other its sums of the rows that the other finishes
+        v4f *const place = reinterpret_cast<v4f *>(lds);
+#pragma unroll
+        for (uint32_t f = 0; f < kKept * PB * 4u; ++f) {
+            const uint32_t q = f / (PB * 4u), r = f / 4u % PB, n = f % 4u;
+            const v16f x = group ? acc[q][r] : acc[kKept + q][r];
+            place[((group * 4u + wave) * kKept * PB * 4u + f) * 64u + lane] = v4f{x[4 * n], x[4 * n + 1], x[4 * n + 2], x[4 * n + 3]};
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t f = 0; f < kKept * PB * 4u; ++f) {
+            const uint32_t q = f / (PB * 4u), r = f / 4u % PB, n = f % 4u;
+            const v4f y = place[(((1u - group) * 4u + wave) * kKept * PB * 4u + f) * 64u + lane];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[q][r][4 * n + e] = (group ? acc[kKept + q][r][4 * n + e] : acc[q][r][4 * n + e]) + y[e];
+        }
+        __syncthreads();
+    }
+    p.out = static_cast<T *>(p.out) + split * p.apart;
     // Results by rows: each wavefront turns its sets of 32 rows round in a part of LDS of its own, so that what a wavefront stores are whole lines.
     constexpr uint32_t kWide = 32 * PB, kPitch = kWide + 4;              // floats to a row
-    static_assert(4 * 32 * kPitch * sizeof(float) <= sizeof(lds), "a part of LDS for each wavefront");
-    float *const own = reinterpret_cast<float *>(lds) + wave * 32u * kPitch;
-    const uint32_t row0 = ((uint32_t)first_a + half_a * PA * 2u) * 16u, col0 = ((uint32_t)first_b + half_b * PB * 2u) * 16u;
+    static_assert(GROUPS * 4 * 32 * kPitch * sizeof(float) <= sizeof(lds), "a part of LDS for each wavefront");
+    float *const own = reinterpret_cast<float *>(lds) + (group * 4u + wave) * 32u * kPitch;
+    const uint32_t row0 = ((uint32_t)first_a + (half_a * PA + kept) * 2u) * 16u, col0 = ((uint32_t)first_b + half_b * PB * 2u) * 16u;
     constexpr int N = 16 / (int)sizeof(T);                               // columns of a lane
     constexpr uint32_t kLanes = kWide / N, kRows = 64u / kLanes;
     const uint32_t mine = lane % kLanes * N;
@@ -264,13 +323,13 @@ __global__ __launch_bounds__(kBlock, BLOCKS) void mx_matmul_lds_k(MxProduct p, u
         for (int e = 0; e < N; ++e) bias[e] = in_global(p.bias)[col0 + mine + e];
     }
 #pragma unroll
-    for (uint32_t q = 0; q < PA; ++q) {
+    for (uint32_t q = 0; q < kKept; ++q) {
 #pragma unroll
         for (uint32_t r = 0; r < PB; ++r)
 #pragma unroll
             for (uint32_t n = 0; n < 4; ++n)
                 *reinterpret_cast<v4f *>(own + (lane & 31u) * kPitch + r * 32u + n * 8u + (lane >> 5) * 4u) =
-                    v4f{acc[q][r][4 * n], acc[q][r][4 * n + 1], acc[q][r][4 * n + 2], acc[q][r][4 * n + 3]};
+                    v4f{sum[q][r][4 * n], sum[q][r][4 * n + 1], sum[q][r][4 * n + 2], sum[q][r][4 * n + 3]};
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         const uint32_t top = row0 + q * 32u;
@@ -299,19 +358,109 @@ __global__ __launch_bounds__(kBlock, BLOCKS) void mx_matmul_lds_k(MxProduct p, u
     }
 }
 
+// ---- splits ---------------------------------------------------------------------------------------------------------------
+// The parts' sums, in their order, and what else a result has: a thread to four columns of a row.
+template <class T>
+__global__ __launch_bounds__(kBlock) void mx_join_k(MxProduct p, uint64_t first, uint32_t splits, uint32_t wide)
+{
+    const uint64_t at = (first + blockIdx.x) * kBlock + threadIdx.x;
+    const uint32_t row = (uint32_t)(at / wide), col = (uint32_t)(at % wide) * 4u;
+    if (row >= p.a.rows) return;
+    const global_ptr<const v4f> from = (global_ptr<const v4f>)in_global(p.partial + ((size_t)row * wide * 4u + col));
+    v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t k = 0; k < splits; k += 4u) {      // (four on their way at once)
+        v4f y[4];
+#pragma unroll
+        for (uint32_t j = 0; j < 4u; ++j) y[j] = from[(size_t)(k + j < splits ? k + j : splits - 1u) * (p.apart / 4u)];
+#pragma unroll
+        for (uint32_t j = 0; j < 4u; ++j) if (k + j < splits) x += y[j];
+    }
+    finish<T>(p, row, col, x);
+}
+// A product whose steps `splits` blocks share: `parts` takes it as one of 32-bit results into the scratch, a part behind the other.
+template <class T, class Parts, class Whole>
+static void shared_by(const LaunchCtx &lc, const MxProduct &p, uint32_t splits, Parts parts, Whole whole)
+{
+    if (splits == 1u) {
+        whole(p);
+        return;
+    }
+    const uint32_t wide = (p.b.rows + 3u) / 4u;
+    MxProduct q = p;
+    q.out = p.partial;
+    q.bias = nullptr;
+    q.accumulate = false;
+    q.stride = (int64_t)wide * 4;
+    q.apart = (size_t)p.a.rows * wide * 4u;
+    parts(q);
+    MxProduct j = p;
+    j.apart = q.apart;
+    in_launches(((uint64_t)p.a.rows * wide + kBlock - 1u) / kBlock, [&](uint64_t first, uint32_t n) { launch(mx_join_k<T>, dim3(n), dim3(kBlock), lc.stream, j, first, splits, wide); });
+}
+
+// How many blocks share a tile's steps: the power of two whose estimate is the shortest, from what was measured: 3 us for a round of 256 blocks to begin and end,
+// `step` us for each of its steps; for the parts' pass 3 us, and 2 us for a million of their elements.  (512 x 1024 outputs over 12 544: 24.8 us
+// without splits, 16.1 with eight; 256 x 256 over 65 536 104 and 21.6; 2048 x 2048 over 4096 14.7 with none.  Parts that the last block of a tile to come adds
+// up, through memory and counts, took 25 us for the first.)
+static uint32_t splits_for(const MxProduct &p, uint64_t tiles, double step)
+{
+    const uint64_t part = (uint64_t)p.a.rows * ((p.b.rows + 3u) / 4u * 4u);
+    uint32_t best = 1;
+    double least = 0.0;
+    for (uint32_t n = 1; n <= 64u && n <= p.a.steps && (n == 1u || n * part <= kMxPartial); n *= 2u) {
+        const double t = (double)((tiles * n + 255u) / 256u) * (3.0 + step * ((p.a.steps + n - 1u) / n)) + (n == 1u ? 0.0 : 3.0 + (double)(n * part) * 2e-6);
+        if (n == 1u || t < least) {
+            least = t;
+            best = n;
+        }
+    }
+    return best;
+}
+template <class T, int MT, int NT>
+static void few_of(const LaunchCtx &lc, const MxProduct &p)
+{
+    const uint64_t tiles_b = (p.b.rows + 16u * NT - 1u) / (16u * NT), tiles = (p.a.rows + 16u * MT - 1u) / (16u * MT) * tiles_b;
+    const uint32_t waves = p.a.steps < kFewWaves ? p.a.steps : kFewWaves, splits = splits_for(p, tiles, 0.04);
+    const auto go = [&](auto k, const MxProduct &q) {
+        in_launches(tiles * splits, [&](uint64_t first, uint32_t n) { launch(k, dim3(n), dim3(waves * 64u), lc.stream, q, first, (uint32_t)tiles_b, splits); });
+    };
+    shared_by<T>(lc, p, splits, [&](const MxProduct &q) { go(mx_matmul_few_k<float, MT, NT>, q); }, [&](const MxProduct &q) { go(mx_matmul_few_k<T, MT, NT>, q); });
+}
+template <class T, int PAIRS, int GROUPS>
+static bool lds_of(const LaunchCtx &lc, const MxProduct &p, uint64_t least)
+{
+    constexpr uint32_t kSide = 64 * PAIRS;
+    const uint64_t ta = (p.a.rows + kSide - 1u) / kSide, tb = (p.b.rows + kSide - 1u) / kSide;
+    if (ta * tb < least || ta * tb >= (1u << 22) || p.a.steps >= (1u << 16)) return false;
+    const uint32_t splits = PAIRS == 4 ? 1u : splits_for(p, ta * tb, 0.2);
+    const auto go = [&](auto k, const MxProduct &q) {
+        launch(k, dim3((uint32_t)(ta * tb) * splits), dim3(kBlock * GROUPS), lc.stream, q, (uint32_t)ta, (uint32_t)tb, splits);
+    };
+    shared_by<T>(lc, p, splits, [&](const MxProduct &q) { go(mx_matmul_lds_k<float, PAIRS, PAIRS, GROUPS>, q); },
+                 [&](const MxProduct &q) { go(mx_matmul_lds_k<T, PAIRS, PAIRS, GROUPS>, q); });
+    return true;
+}
+// Which form takes a product (us, 16-bit results):
+//   256 x 256 outputs to a block    where that makes 110 blocks: 2048 x 2560 (80) over 4096 32 and 25 by the next form, 3328 x 2560 (130) over 2048 23 and 26
+//   128 x 128                       from 65 rows on: 128 x 4096 over 4096 11.3, and 14 to 20 by the next form, whose blocks read their operands so much oftener
+//   16 to 64 rows                   64 columns to a block where there are 200 such blocks (1 x 32064 over 4096 14.3, 5 TB/s), else 32 or 16: 16 x 4096 over
+//                                   4096 7.0, and 10 with 64
 template <class T>
 static void matmul_of(const LaunchCtx &lc, const MxProduct &p)
 {
-    if (p.a.rows > 128u && p.a.steps < (1u << 16)) {
-        const uint32_t ta = (p.a.rows + 255u) / 256u, tb = (p.b.rows + 255u) / 256u;
-        if ((uint64_t)ta * tb < (1u << 23)) {
-            if (getenv("T4")) { const uint32_t tb = (p.b.rows + 127u) / 128u; launch(mx_matmul_lds_k<T, 4, 2, 3, 2>, dim3(ta * tb), dim3(kBlock), lc.stream, p, ta, tb); }
-            else launch(mx_matmul_lds_k<T, 4, 4, 4, 1>, dim3(ta * tb), dim3(kBlock), lc.stream, p, ta, tb);
-            return;
-        }
+    if (p.a.rows > 64u && (lds_of<T, 4, 1>(lc, p, 110u) || lds_of<T, 2, 2>(lc, p, 1u))) return;
+    const bool wide = p.b.rows > 64u * 200u;
+    if (p.a.rows <= 16u) {
+        if (wide) few_of<T, 1, 4>(lc, p);
+        else if (p.b.rows > 32u * 200u) few_of<T, 1, 2>(lc, p);
+        else few_of<T, 1, 1>(lc, p);
+    } else if (p.a.rows <= 32u) {
+        if (wide) few_of<T, 2, 4>(lc, p);
+        else few_of<T, 2, 1>(lc, p);
+    } else {
+        if (wide) few_of<T, 4, 4>(lc, p);
+        else few_of<T, 4, 1>(lc, p);
     }
-    const uint32_t tiles_a = (p.a.rows + 127u) / 128u, tiles_b = (p.b.rows + 127u) / 128u;
-    in_launches((uint64_t)tiles_a * tiles_b, [&](uint64_t first, uint32_t n) { launch(mx_matmul_k<T>, dim3(n), dim3(kBlock), lc.stream, p, first, tiles_b); });
 }
 void launch_mx_matmul(const LaunchCtx &lc, int dtype, const MxProduct &p)
 {

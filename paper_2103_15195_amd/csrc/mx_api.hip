@@ -20,7 +20,6 @@ struct mc_step8 {
 struct mc_mx {
     int device = 0;
     float *d_partial = nullptr;
-    uint32_t *d_counts = nullptr;        // 0 between calls
 };
 
 namespace {
@@ -146,7 +145,6 @@ int mc_mx_destroy(mc_mx *h)
         OnDevice guard(h->device);
         (void)hipDeviceSynchronize();
         if (h->d_partial) (void)hipFree(h->d_partial);
-        if (h->d_counts) (void)hipFree(h->d_counts);
     }
     delete h;
     return MC_OK;
@@ -160,9 +158,6 @@ int mc_mx_create(mc_mx **out)
     if (!h) return MC_ERR_ALLOC;
     if (hipGetDevice(&h->device) != hipSuccess) { (void)hipGetLastError(); delete h; return MC_ERR_DEVICE; }
     int rc = grab(&h->d_partial, kMxPartial * sizeof(float));
-    if (rc == MC_OK) rc = grab(&h->d_counts, kMxCounts * sizeof(uint32_t));
-    // (done before work on any stream)
-    if (rc == MC_OK && (hipMemset(h->d_counts, 0, kMxCounts * sizeof(uint32_t)) != hipSuccess || hipDeviceSynchronize() != hipSuccess)) rc = MC_ERR_DEVICE;
     if (rc != MC_OK) { (void)hipGetLastError(); mc_mx_destroy(h); return rc; }
     *out = h;
     return MC_OK;
@@ -214,7 +209,7 @@ int mc_mx_matmul(mc_mx *h, const mc_mx_matrix *a, const mc_mx_matrix *b, const m
     MxProduct p = {};
     p.a = view(a); p.b = view(b);
     p.out = y->out; p.bias = y->bias; p.stride = y->stride; p.accumulate = y->accumulate != 0;
-    p.partial = h->d_partial; p.counts = h->d_counts;
+    p.partial = h->d_partial;
     launch_mx_matmul(on(stream), y->dtype, p);
     return launched();
 }

@@ -37,16 +37,16 @@ struct MxProduct {
     int64_t stride;
     bool accumulate;
     float *partial;                          // kMxPartial floats
-    uint32_t *counts;                        // kMxCounts, 0 between calls
+    size_t apart;                            // elements from a part's result to the next one's
 };
-constexpr size_t kMxPartial = size_t(1) << 24, kMxCounts = 4096;
+constexpr size_t kMxPartial = size_t(1) << 24;
 void launch_mx_matmul(const LaunchCtx &lc, int dtype, const MxProduct &p);
 
-// Blocks of 256 threads in launches of fewer than 2^32 threads: body(first block, blocks).
+// Blocks of up to 512 threads in launches of fewer than 2^32 threads: body(first block, blocks).
 template <class Body>
 inline void in_launches(uint64_t blocks, Body body)
 {
-    constexpr uint64_t most = 1u << 23;
+    constexpr uint64_t most = 1u << 22;
     for (uint64_t first = 0; first < blocks; first += most) body(first, (uint32_t)(blocks - first < most ? blocks - first : most));
 }
 

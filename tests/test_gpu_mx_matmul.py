@@ -54,6 +54,43 @@ def test_exact_sums(shape, dtype):
     h.close()
 
 
+@pytest.mark.parametrize("shape", [(5, 30, 40000), (40, 33, 50000), (70, 100, 20000), (130, 70, 9000), (2700, 2600, 300), (2817, 2561, 130), (9, 13000, 700), (30, 12900, 300), (50, 13001, 260)], ids=str)
+def test_large_and_long(shape):
+    """Sums that several blocks share, and outputs of many blocks, in each of the forms."""
+    (m, n, k), h = shape, X.Mx()
+    rng = np.random.default_rng(m + n + k)
+    a, b = grid(rng, m, k), grid(rng, n, k)
+    want = (a @ b.t()).float()
+    bias = torch.from_numpy(rng.integers(-64, 64, n) / 4.0).float()
+    A, Bm = held(a), held(b)
+    for kind in (torch.float32, torch.bfloat16):
+        out = torch.empty(m, n, dtype=kind, device=DEV)
+        h.mc_mx_matmul(A, Bm, out)
+        assert torch.equal(out.cpu(), want.to(kind))
+        h.mc_mx_matmul(A, Bm, out, bias=bias.to(DEV), accumulate=True)
+        assert torch.equal(out.cpu(), (want.to(kind).double() + want.double() + bias.double()).float().to(kind))
+
+
+def test_very_long_sums():
+    """More steps than the forms through LDS take."""
+    h, (m, n, k) = X.Mx(), (66, 3, 2 ** 23 + 133)
+    a, b = torch.zeros(m, k, dtype=torch.bfloat16, device=DEV), torch.zeros(n, k, dtype=torch.bfloat16, device=DEV)
+    at = [0, 2 ** 23 - 1, 2 ** 23, k - 1]
+    for i, c in enumerate(at):
+        a[:, c], b[:, c] = float(2 ** i), 1.0
+    a[65], b[2] = 2 * a[0], 4 * b[0]
+    A, Bm, out = X.MxMatrix(m, k), X.MxMatrix(n, k), torch.empty(m, n, device=DEV)
+    h.mc_mx_quantize(a, by_rows=A)
+    h.mc_mx_quantize(b, by_rows=Bm)
+    h.mc_mx_matmul(A, Bm, out)
+    want = torch.full((m, n), 15.0)
+    want[65] *= 2
+    want[:, 2] *= 4
+    assert torch.equal(out.cpu(), want)
+    del a, b, A, Bm
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("shape", [(1, 70, 5000), (40, 70, 3000), (130, 260, 1500)], ids=str)
 def test_rounded_sums(shape):
     """Scales over a wide range.  Each of the steps' sums of 128 products and the additions that join them is off by at most a few units of its terms' size: a
