@@ -384,9 +384,8 @@ PyObject *norm_by(PyObject *self, PyObject *const *a, Py_ssize_t n, bool clip)
 PyObject *grad_norm(PyObject *self, PyObject *const *a, Py_ssize_t n) { return norm_by(self, a, n, false); }
 PyObject *grad_clip(PyObject *self, PyObject *const *a, Py_ssize_t n) { return norm_by(self, a, n, true); }
 // (handle, step, lr, beta1, beta2, eps, weight_decay, coefficient or None, the stream's callable)
-PyObject *adamw(PyObject *self, PyObject *const *a, Py_ssize_t n)
+PyObject *adamw_by(const StepCalls *c, adamw_fn fn, PyObject *const *a, Py_ssize_t n)
 {
-    const StepCalls *c = reinterpret_cast<const StepCalls *>(self);
     void *handle, *stream;
     const void *coef;
     Adamw w;
@@ -401,9 +400,14 @@ PyObject *adamw(PyObject *self, PyObject *const *a, Py_ssize_t n)
     if (!vector(c, a[7], 1, c->kinds[0], &coef, true) || !stream_here(c, a[8], &stream)) return other();
     int rc;
     Py_BEGIN_ALLOW_THREADS
-    rc = c->adamw(handle, &w, coef, stream);
+    rc = fn(handle, &w, coef, stream);
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
+}
+PyObject *adamw(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const StepCalls *c = reinterpret_cast<const StepCalls *>(self);
+    return adamw_by(c, c->adamw, a, n);
 }
 // StepCalls(float32, bfloat16, float16, int64, addresses of mc_token_logp, mc_policy_loss, mc_grad_norm, mc_grad_clip, mc_adamw)
 PyObject *step_calls_new(PyTypeObject *type, PyObject *args, PyObject *)
@@ -451,9 +455,127 @@ void step_calls_gone(PyObject *self)
     Py_TYPE(self)->tp_free(self);
 }
 
+// ---- a step in few bits (mx.py) --------------------------------------------------------------------------------------------------------------
+// The structures of mergecomp_mx.h.
+struct Matrix {
+    void *codes, *scales;
+    int64_t rows, cols;
+};
+struct Source {
+    const void *data;
+    int64_t rows, cols, stride;
+    int32_t dtype;
+};
+struct Result {
+    void *out;
+    int64_t stride;
+    int32_t dtype, accumulate;
+    const void *bias;
+};
+typedef int (*quantize_fn)(void *, const Source *, const Matrix *, const Matrix *, void *, int64_t, void *);
+typedef int (*matmul_fn)(void *, const Matrix *, const Matrix *, const Result *, void *);
+
+PyObject *g_at, *g_index;             // names
+
+// The entry points, and the type of quantised matrices, whose structure lies at the attribute `_at` and whose device has the index `_index`.
+struct MxCalls {
+    StepCalls base;                   // types and device
+    PyTypeObject *matrix;
+    quantize_fn quantize;
+    matmul_fn matmul;
+    adamw_fn adamw8;
+};
+bool quantised(const MxCalls *c, PyObject *o, const Matrix **m)
+{
+    if (Py_TYPE(o) != c->matrix) return false;
+    PyObject *i = PyObject_GetAttr(o, g_index), *a = i ? PyObject_GetAttr(o, g_at) : nullptr;
+    void *p = nullptr;
+    const bool ok = a && PyLong_Check(i) && PyLong_AsLong(i) == c->base.device && address(a, &p) && p;
+    Py_XDECREF(i);
+    Py_XDECREF(a);
+    *m = static_cast<const Matrix *>(p);
+    return ok;
+}
+// (handle, x, by_rows or None, by_cols or None, values or None, the stream's callable)
+PyObject *quantize(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const MxCalls *c = reinterpret_cast<const MxCalls *>(self);
+    void *handle, *stream, *at, *values = nullptr;
+    const Matrix *rows = nullptr, *cols = nullptr;
+    int64_t size[2], vsize[2], vstride = 0;
+    Source x;
+    if (n != 6 || !address(a[0], &handle)) return other();
+    x.dtype = matrix(&c->base, a[1], size, &x.stride, &at);
+    if (x.dtype < 0) return other();
+    x.data = at;
+    x.rows = size[0];
+    x.cols = size[1];
+    if (a[2] != Py_None && (!quantised(c, a[2], &rows) || rows->rows != x.rows || rows->cols != x.cols)) return other();
+    if (a[3] != Py_None && (!quantised(c, a[3], &cols) || cols->rows != x.cols || cols->cols != x.rows)) return other();
+    if (a[4] != Py_None && (matrix(&c->base, a[4], vsize, &vstride, &values) != x.dtype || vsize[0] != x.rows || vsize[1] != x.cols)) return other();
+    if (!stream_here(&c->base, a[5], &stream)) return other();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = c->quantize(handle, &x, rows, cols, values, vstride, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+// (handle, a, b, out, bias or None, accumulate, the stream's callable)
+PyObject *matmul(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const MxCalls *c = reinterpret_cast<const MxCalls *>(self);
+    void *handle, *stream, *out;
+    const Matrix *x, *w;
+    int64_t size[2];
+    Result y;
+    if (n != 7 || !address(a[0], &handle) || !quantised(c, a[1], &x) || !quantised(c, a[2], &w) || (a[5] != Py_False && a[5] != Py_True)) return other();
+    y.dtype = matrix(&c->base, a[3], size, &y.stride, &out);
+    if (y.dtype < 0 || size[0] != x->rows || size[1] != w->rows || x->cols != w->cols) return other();
+    y.out = out;
+    y.accumulate = a[5] == Py_True;
+    if (!vector(&c->base, a[4], size[1], c->base.kinds[0], &y.bias, true) || !stream_here(&c->base, a[6], &stream)) return other();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = c->matmul(handle, x, w, &y, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+PyObject *adamw8(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    const MxCalls *c = reinterpret_cast<const MxCalls *>(self);
+    return adamw_by(&c->base, c->adamw8, a, n);
+}
+// MxCalls(float32, bfloat16, float16, the matrices' type, device index, addresses of mc_mx_quantize, mc_mx_matmul, mc_adamw8)
+PyObject *mx_calls_new(PyTypeObject *type, PyObject *args, PyObject *)
+{
+    PyObject *kinds[3] = {}, *matrix = nullptr;
+    long device = 0;
+    unsigned long long at[3] = {};
+    if (!PyArg_ParseTuple(args, "OOOO!lKKK", &kinds[0], &kinds[1], &kinds[2], &PyType_Type, &matrix, &device, &at[0], &at[1], &at[2])) return nullptr;
+    MxCalls *c = reinterpret_cast<MxCalls *>(type->tp_alloc(type, 0));
+    if (!c) return nullptr;
+    for (int k = 0; k < 3; ++k) Py_INCREF(c->base.kinds[k] = kinds[k]);
+    Py_INCREF(matrix);
+    c->matrix = reinterpret_cast<PyTypeObject *>(matrix);
+    c->base.device = device;
+    c->quantize = (quantize_fn)(uintptr_t)at[0];
+    c->matmul = (matmul_fn)(uintptr_t)at[1];
+    c->adamw8 = (adamw_fn)(uintptr_t)at[2];
+    return reinterpret_cast<PyObject *>(c);
+}
+void mx_calls_gone(PyObject *self)
+{
+    MxCalls *c = reinterpret_cast<MxCalls *>(self);
+    for (PyObject *k : c->base.kinds) Py_XDECREF(k);
+    Py_XDECREF(reinterpret_cast<PyObject *>(c->matrix));
+    Py_TYPE(self)->tp_free(self);
+}
+
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef calls_methods[] = {FAST(compress), FAST(compress_static), FAST(decompress), FAST(compress_groups), FAST(decompress_groups), {nullptr, nullptr, 0, nullptr}};
 PyMethodDef step_calls_methods[] = {FAST(token_logp), FAST(policy_loss), FAST(grad_norm), FAST(grad_clip), FAST(adamw), {"on", on, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+PyMethodDef mx_calls_methods[] = {FAST(quantize), FAST(matmul), FAST(adamw8), {nullptr, nullptr, 0, nullptr}};
+PyTypeObject MxCallsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 PyTypeObject CallsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 PyTypeObject StepCallsType = {PyVarObject_HEAD_INIT(nullptr, 0)};
 PyTypeObject RawStreamType = {PyVarObject_HEAD_INIT(nullptr, 0)};
@@ -463,7 +585,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", "The hot calls of the 
 
 PyMODINIT_FUNC PyInit__fastcall(void)
 {
-    const struct { PyObject **at; const char *name; } names[] = {{&g_data_ptr, "data_ptr"}, {&g_dtype, "dtype"}, {&g_is_cuda, "is_cuda"}, {&g_get_device, "get_device"}, {&g_shape, "shape"}, {&g_stride, "stride"}};
+    const struct { PyObject **at; const char *name; } names[] = {{&g_data_ptr, "data_ptr"}, {&g_dtype, "dtype"}, {&g_is_cuda, "is_cuda"}, {&g_get_device, "get_device"}, {&g_shape, "shape"}, {&g_stride, "stride"}, {&g_at, "_at"}, {&g_index, "_index"}};
     for (const auto &n : names) if (!*n.at && !(*n.at = PyUnicode_InternFromString(n.name))) return nullptr;
     CallsType.tp_name = "_fastcall.Calls";
     CallsType.tp_basicsize = sizeof(Calls);
@@ -483,10 +605,17 @@ PyMODINIT_FUNC PyInit__fastcall(void)
     StepCallsType.tp_new = step_calls_new;
     StepCallsType.tp_dealloc = step_calls_gone;
     StepCallsType.tp_methods = step_calls_methods;
-    if (PyType_Ready(&CallsType) < 0 || PyType_Ready(&RawStreamType) < 0 || PyType_Ready(&StepCallsType) < 0) return nullptr;
+    MxCallsType.tp_name = "_fastcall.MxCalls";
+    MxCallsType.tp_basicsize = sizeof(MxCalls);
+    MxCallsType.tp_flags = Py_TPFLAGS_DEFAULT;
+    MxCallsType.tp_new = mx_calls_new;
+    MxCallsType.tp_dealloc = mx_calls_gone;
+    MxCallsType.tp_methods = mx_calls_methods;
+    if (PyType_Ready(&MxCallsType) < 0 || PyType_Ready(&CallsType) < 0 || PyType_Ready(&RawStreamType) < 0 || PyType_Ready(&StepCallsType) < 0) return nullptr;
     PyObject *m = PyModule_Create(&module);
     if (!m) return nullptr;
     if (PyModule_AddObjectRef(m, "Calls", reinterpret_cast<PyObject *>(&CallsType)) < 0 ||
+        PyModule_AddObjectRef(m, "MxCalls", reinterpret_cast<PyObject *>(&MxCallsType)) < 0 ||
         PyModule_AddObjectRef(m, "StepCalls", reinterpret_cast<PyObject *>(&StepCallsType)) < 0 ||
         PyModule_AddObjectRef(m, "RawStream", reinterpret_cast<PyObject *>(&RawStreamType)) < 0) { Py_DECREF(m); return nullptr; }
     return m;

@@ -57,6 +57,25 @@ def lib():
     return L
 
 
+class _NoFastCalls:
+    """Stands for the extension module's calls where there is no module: no argument is in a form that it takes."""
+
+    @staticmethod
+    def quantize(*args):
+        return None
+    matmul = adamw8 = quantize
+
+
+def _fast(device):
+    """The extension module's calls for tensors on a device."""
+    L = lib()
+    try:
+        return B._fastcall().MxCalls(torch.float32, torch.bfloat16, torch.float16, MxMatrix, device.index,
+                                     *[C.cast(f, C.c_void_p).value for f in (L.mc_mx_quantize, L.mc_mx_matmul, L.mc_adamw8)])
+    except ImportError:                          # (the library's own loading has warned)
+        return _NoFastCalls()
+
+
 class Step8:
     """One model's list of tensors whose moments are held in 8 bits, on the current device: wraps mc_step8.  All that is handed over later has to
     be on that device.
@@ -79,15 +98,19 @@ class Step8:
                        "exp_avg_scale": torch.float32, "exp_avg_sq_scale": torch.float32}
         self._kept = {}
         self._h = C.c_void_p()
+        self._at = 0                             # the same as an int
         nm = (C.c_int64 * max(n, 1))(*self.numel)
         nd = None if no_decay is None else (C.c_uint8 * max(n, 1))(*[1 if x else 0 for x in no_decay])
         B._check(lib().mc_step8_create(C.byref(self._h), nm, n, grad, model, nd), "mc_step8_create")
+        self._at = self._h.value
         self._device = torch.device("cuda", torch.cuda.current_device())
+        self._fast = _fast(self._device)
 
     def close(self) -> None:
         if getattr(self, "_h", None):
             lib().mc_step8_destroy(self._h)
             self._h = None
+            self._at = 0
             self._kept = {}
 
     def __del__(self):
@@ -127,8 +150,10 @@ class Step8:
     def mc_adamw8(self, step: int, lr: float, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
                   coef=None, stream=None) -> None:
         """coef: one float on the device that the gradients are multiplied by, such as the second of mc_grad_norm."""
-        cfg = S.McAdamwConfig(lr, betas[0], betas[1], eps, weight_decay, step)
-        rc = lib().mc_adamw8(self._h, C.byref(cfg), None if coef is None else S._vector(coef, "coef", 1, self._device), S._stream_on(stream, self._device))
+        rc = self._fast.adamw8(self._at, step, lr, betas[0], betas[1], eps, weight_decay, coef, B._raw_stream) if stream is None else None
+        if rc is None:
+            cfg = S.McAdamwConfig(lr, betas[0], betas[1], eps, weight_decay, step)
+            rc = lib().mc_adamw8(self._h, C.byref(cfg), None if coef is None else S._vector(coef, "coef", 1, self._device), S._stream_on(stream, self._device))
         if rc:
             raise B.McError(rc, "mc_adamw8")
 
@@ -152,7 +177,8 @@ class MxMatrix:
                 raise ValueError(f"{name}: {n} contiguous bytes on one device, not {tuple(t.shape)} of {t.dtype} on {t.device}")
         self.codes, self.scales = codes, scales
         self._c = McMxMatrix(codes.data_ptr(), scales.data_ptr(), self.rows, self.cols)
-        self._device = codes.device
+        self._at = C.addressof(self._c)
+        self._device, self._index = codes.device, codes.device.index
 
 
 def _matrix(m, name: str, device, rows=None, cols=None):
@@ -167,13 +193,17 @@ class Mx:
 
     def __init__(self):
         self._h = C.c_void_p()
+        self._at = 0                             # the same as an int
         B._check(lib().mc_mx_create(C.byref(self._h)), "mc_mx_create")
+        self._at = self._h.value
         self._device = torch.device("cuda", torch.cuda.current_device())
+        self._fast = _fast(self._device)
 
     def close(self) -> None:
         if getattr(self, "_h", None):
             lib().mc_mx_destroy(self._h)
             self._h = None
+            self._at = 0
 
     def __del__(self):
         try:
@@ -184,6 +214,14 @@ class Mx:
     def mc_mx_quantize(self, x, by_rows=None, by_cols=None, values=None, stream=None) -> None:
         """x: rows of contiguous values.  by_rows: an MxMatrix of x's shape; by_cols: one of the transposed shape; values: of x's shape and type (it may be
         x), what by_rows stands for."""
+        rc = self._fast.quantize(self._at, x, by_rows, by_cols, values, B._raw_stream) if stream is None else None
+        if rc is None:
+            rc = self._quantize(x, by_rows, by_cols, values, S._stream_on(stream, self._device))
+        if rc:
+            raise B.McError(rc, "mc_mx_quantize")
+
+    def _quantize(self, x, by_rows, by_cols, values, stream) -> int:
+        """The same through ctypes, which says what is wrong with an argument."""
         rows, cols, stride = S._rows(x, "x", self._device)
         at, vstride = None, 0
         if values is not None:
@@ -194,17 +232,21 @@ class Mx:
         src = McMxSource(x.data_ptr(), rows, cols, stride, S.DTYPE_IDS[x.dtype])
         r = None if by_rows is None else _matrix(by_rows, "by_rows", self._device, rows, cols)
         c = None if by_cols is None else _matrix(by_cols, "by_cols", self._device, cols, rows)
-        rc = lib().mc_mx_quantize(self._h, C.byref(src), r, c, at, vstride, S._stream_on(stream, self._device))
-        if rc:
-            raise B.McError(rc, "mc_mx_quantize")
+        return lib().mc_mx_quantize(self._h, C.byref(src), r, c, at, vstride, stream)
 
     def mc_mx_matmul(self, a, b, out, bias=None, accumulate: bool = False, stream=None) -> None:
         """out = a b^T (+ bias, b.rows floats) (+ out as it was), out: a.rows rows of b.rows contiguous values."""
+        rc = self._fast.matmul(self._at, a, b, out, bias, accumulate, B._raw_stream) if stream is None else None
+        if rc is None:
+            rc = self._matmul(a, b, out, bias, accumulate, S._stream_on(stream, self._device))
+        if rc:
+            raise B.McError(rc, "mc_mx_matmul")
+
+    def _matmul(self, a, b, out, bias, accumulate, stream) -> int:
+        """The same through ctypes, which says what is wrong with an argument."""
         pa, pb = _matrix(a, "a", self._device), _matrix(b, "b", self._device)
         rows, cols, stride = S._rows(out, "out", self._device)
         if rows != a.rows or cols != b.rows or a.cols != b.cols:
             raise ValueError(f"out: {a.rows} x {b.rows} of sums over {a.cols} and {b.cols} columns, not {rows} x {cols}")
         y = McMxResult(out.data_ptr(), stride, S.DTYPE_IDS[out.dtype], 1 if accumulate else 0, None if bias is None else S._vector(bias, "bias", cols, self._device))
-        rc = lib().mc_mx_matmul(self._h, pa, pb, C.byref(y), S._stream_on(stream, self._device))
-        if rc:
-            raise B.McError(rc, "mc_mx_matmul")
+        return lib().mc_mx_matmul(self._h, pa, pb, C.byref(y), stream)
