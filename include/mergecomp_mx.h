@@ -105,7 +105,7 @@ int mc_mx_quantize(mc_mx *h, const mc_mx_source *x, const mc_mx_matrix *by_rows,
 
 /*
  * out[i][j] = sum_k a[i][k] b[j][k]  (+ bias[j])  (+ out[i][j] as it was, with `accumulate`)
- * Products and scales are exact, sums binary32; the result is rounded once, to nearest even.
+ * Products and scales are exact, sums binary32 (what is below 2^-126 may count as 0); the result is rounded once, to nearest even.
  *   a          m x k, such as activations            b   n x k, such as weights of n outputs
  *   out        dtype, row i from out + i * stride elements on
  *   bias       device, n floats; may be NULL

@@ -160,10 +160,15 @@ class Step8:
 
 class MxMatrix:
     """rows x cols values in microscaled 4-bit floating point: the two buffers of mc_mx_matrix, made here (on the current device) or
-    handed over (bytes, contiguous, on one device, of code_bytes and scale_bytes)."""
+    handed over (bytes, contiguous, on one device, mc_mx_code_bytes and mc_mx_scale_bytes of them).  A matrix keeps its buffers: another one's are another matrix."""
+
+    rows = property(lambda self: self._rows)
+    cols = property(lambda self: self._cols)
+    codes = property(lambda self: self._codes)
+    scales = property(lambda self: self._scales)
 
     def __init__(self, rows: int, cols: int, codes=None, scales=None):
-        self.rows, self.cols = int(rows), int(cols)
+        self._rows, self._cols = int(rows), int(cols)
         if self.rows < 0 or self.cols < 1 or max(self.rows, self.cols) >= 2 ** 31 - 2 ** 16:
             raise ValueError(f"{rows} x {cols}: rows from 0 and columns from 1 on, below 2^31 - 2^16")
         if (codes is None) != (scales is None):
@@ -175,7 +180,7 @@ class MxMatrix:
         for name, t, n in (("codes", codes, sizes[0]), ("scales", scales, sizes[1])):
             if t.dtype is not torch.uint8 or t.numel() != n or not t.is_contiguous() or t.device != codes.device or not t.is_cuda:
                 raise ValueError(f"{name}: {n} contiguous bytes on one device, not {tuple(t.shape)} of {t.dtype} on {t.device}")
-        self.codes, self.scales = codes, scales
+        self._codes, self._scales = codes, scales
         self._c = McMxMatrix(codes.data_ptr(), scales.data_ptr(), self.rows, self.cols)
         self._at = C.addressof(self._c)
         self._device, self._index = codes.device, codes.device.index

@@ -150,7 +150,11 @@ def test_matrices():
         with pytest.raises(ValueError):
             X.MxMatrix(rows, cols, Tensor((0,), torch.uint8), Tensor((0,), torch.uint8))
     good = Tensor((2048,), torch.uint8), Tensor((256,), torch.uint8)
-    assert X.MxMatrix(20, 100, *good).cols == 100
+    m = X.MxMatrix(20, 100, *good)
+    assert (m.rows, m.cols, m.codes, m.scales) == (20, 100, *good)
+    for name in ("rows", "cols", "codes", "scales"):          # the library has their addresses
+        with pytest.raises(AttributeError):
+            setattr(m, name, None)
     for codes, scales in ((good[0], None), (None, good[1]), (good[1], good[0]), (good[0], Tensor((256,), torch.uint8, at=0)), (Tensor((2048,), torch.uint8, at=-1), good[1]),
                           (good[0], Tensor((256,), torch.int8))):
         with pytest.raises(ValueError):
