@@ -84,7 +84,7 @@ __device__ __forceinline__ float hold8(const float (&x)[8], codes8 &c)
         for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]) < __builtin_huge_valf() ? fabsf(x[e]) : 0.0f);
     }
     top = row_max(top);
-    const float scale = top >= 0x1p-100f ? top * (1.0f / 448.0f) : 0.0f, back = scale > 0.0f ? __builtin_amdgcn_rcpf(scale) : 0.0f;
+    const float scale = top >= 0x1p-100f ? top * (1.0f / 448.0f) : 0.0f, back = scale > 0.0f ? 1.0f / scale : 0.0f;
     const float least = ROOT && scale > 0.0f ? 0x1p-9f : 0.0f;
     float y[8];
 #pragma unroll
@@ -106,9 +106,20 @@ __device__ __forceinline__ global_ptr<T> list8(const Step8View &v, uint32_t list
 {
     return in_global(reinterpret_cast<T *>(ld_uniform(v.addr + (size_t)list * v.tensors + tensor)));
 }
-// Root and quotient are the hardware's, off by a unit in the last place each: the correctly rounded ones are about 25 instructions an element more.
-// With those, and every access under a condition of its own, 25.6 M elements in 32 bits took 119 us, 160 M of mixed precision 652; so 80 (5.2 TB/s) and
-// 471 (5.5 TB/s), which is the memory's rate: AdamW in 32 bits moves 5.5 and 5.8 TB/s.
+// The square root, rounded correctly from 2^-96 on (below, by up to a unit in the last place): the hardware's, or the number on either side of it where
+// the square of half way to that one says so.
+__device__ __forceinline__ float root_of(float x)
+{
+    const float s = __builtin_amdgcn_sqrtf(x);
+    const float under = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, s) - 1u), over = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, s) + 1u);
+    float r = __builtin_fmaf(-under, s, x) <= 0.0f ? under : s;
+    r = __builtin_fmaf(-over, s, x) > 0.0f ? over : r;
+    return x >= 0x1p-126f && x < __builtin_huge_valf() ? r : s;
+}
+// The moments are rounded after every operation, as their formulas stand, so that their codes do not depend on how a compiler joins them: a unit in the last place can
+// decide between two codes.  The weights' quotient is the hardware's reciprocal, off by such a unit.
+// (All accesses under conditions of their own, library root and division: 25.6 M elements in 32 bits 119 us, 160 M of mixed precision 652.  So: 80 (5.2 TB/s) and 467
+// (5.5 TB/s), which is the memory's rate: AdamW in 32 bits moves 5.5 and 5.8 TB/s.  With the hardware's root and fused sums 80 and 471.)
 template <class T, class M, bool FULL>
 __device__ __forceinline__ void adamw8_piece(const Step8View &v, const AdamwArgs &a, uint32_t name, uint32_t index, int32_t hi)
 {
@@ -134,8 +145,8 @@ __device__ __forceinline__ void adamw8_piece(const Step8View &v, const AdamwArgs
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         g[e] *= coef;
-        m[e] = __builtin_fmaf(a.beta1, m[e], a.one_minus_beta1 * g[e]);
-        r[e] = __builtin_amdgcn_sqrtf(__builtin_fmaf(a.beta2 * r[e], r[e], a.one_minus_beta2 * (g[e] * g[e])));
+        m[e] = a.beta1 * m[e] + a.one_minus_beta1 * g[e];
+        r[e] = root_of(a.beta2 * (r[e] * r[e]) + a.one_minus_beta2 * (g[e] * g[e]));
         // (the least normal number, so that its reciprocal is finite)
         const float under = __builtin_fmaf(r[e], a.root, a.eps), q = m[e] * __builtin_amdgcn_rcpf(under < 0x1p-126f ? 0x1p-126f : under);
         w[e] = __builtin_fmaf(-a.rate, q, decay * w[e]);
