@@ -190,43 +190,36 @@ __device__ __forceinline__ void put_codes(const MxView &m, uint32_t row, uint32_
 }
 
 // ---- along the rows ----------------------------------------------------------------------------------------------------
-// 64 rows by 128 columns to a block.  A thread has the same columns of the same row of each of the four tiles of 16 rows (of 32-bit values: of two rows),
-// so that it has a word of scales together.
+// 64 rows by 128 columns to a block.  A thread has the same columns of the same row of each of the four tiles of 16 rows, so that it has a word of scales
+// together.
+template <class T> constexpr uint32_t kRowsThreads = 16u * kRowLanes<T>;
 template <class T, bool VALUES>
-__global__ __launch_bounds__(kBlock) void mx_rows_k(MxSource s, uint64_t first, uint32_t steps)
+__global__ __launch_bounds__(kRowsThreads<T>) void mx_rows_k(MxSource s, uint64_t first, uint32_t steps)
 {
-    constexpr uint32_t kAtOnce = kBlock / kRowLanes<T>, kTurns = 16u / kAtOnce;
     const uint64_t at = first + blockIdx.x;
-    const uint32_t step = (uint32_t)(at % steps), base = (uint32_t)(at / steps) * 64u;
-    const uint32_t lane = threadIdx.x % kRowLanes<T>, sub = threadIdx.x / kRowLanes<T>, col = step * kMxStep + lane * kHas<T>;
+    const uint32_t step = (uint32_t)(at % steps), lane = threadIdx.x % kRowLanes<T>, col = step * kMxStep + lane * kHas<T>;
+    const uint32_t row0 = (uint32_t)(at / steps) * 64u + threadIdx.x / kRowLanes<T>;
     const T *x = static_cast<const T *>(s.x);
     const bool full = step * kMxStep + kMxStep <= s.cols;                // (of columns)
-    codes4 w[kTurns][4];
+    codes4 w[4];
 #pragma unroll
-    for (uint32_t t = 0; t < kTurns; ++t)
+    for (uint32_t q = 0; q < 4; ++q) {
+        w[q] = codes4{0u, 0u, 0u, 0u};
+        if (row0 + q * 16u < s.rows) w[q] = load_words<T, 4>(x + (int64_t)(row0 + q * 16u) * s.stride, col, s.cols, full);
+    }
+    uint32_t scales = 0, scale;
 #pragma unroll
-        for (uint32_t q = 0; q < 4; ++q) {
-            const uint32_t row = base + q * 16u + t * kAtOnce + sub;
-            w[t][q] = codes4{0u, 0u, 0u, 0u};
-            if (row < s.rows) w[t][q] = load_words<T, 4>(x + (int64_t)row * s.stride, col, s.cols, full);
-        }
-#pragma unroll
-    for (uint32_t t = 0; t < kTurns; ++t) {
-        const uint32_t row0 = base + t * kAtOnce + sub;
-        uint32_t scales = 0, scale;
-#pragma unroll
-        for (uint32_t q = 0; q < 4; ++q) {
-            const uint32_t row = row0 + q * 16u, c = row_codes<T, 4>(w[t][q], scale);
-            scales |= scale << (8u * q);
-            if (row >= s.rows) continue;
-            if (s.by_rows.codes) put_codes<T>(s.by_rows, row, step, lane, c);
-            if constexpr (VALUES) store_words<T, 4>(static_cast<T *>(s.values) + (int64_t)row * s.values_stride, col, s.cols, values_of<T, 4>(c, scale));
-        }
-        if (s.by_rows.codes && lane % kBlockLanes<T> == 0 && row0 < s.rows) {
-            const global_ptr<uint8_t> to = in_global(s.by_rows.scales) + scales_at(s.by_rows, row0, step, lane / kBlockLanes<T>);
-            if (row0 + 48u < s.rows) *(global_ptr<uint32_t>)to = scales;
-            else for (uint32_t q = 0; q < 4; ++q) if (row0 + q * 16u < s.rows) to[q] = (uint8_t)(scales >> (8u * q));
-        }
+    for (uint32_t q = 0; q < 4; ++q) {
+        const uint32_t row = row0 + q * 16u, c = row_codes<T, 4>(w[q], scale);
+        scales |= scale << (8u * q);
+        if (row >= s.rows) continue;
+        if (s.by_rows.codes) put_codes<T>(s.by_rows, row, step, lane, c);
+        if constexpr (VALUES) store_words<T, 4>(static_cast<T *>(s.values) + (int64_t)row * s.values_stride, col, s.cols, values_of<T, 4>(c, scale));
+    }
+    if (s.by_rows.codes && lane % kBlockLanes<T> == 0 && row0 < s.rows) {
+        const global_ptr<uint8_t> to = in_global(s.by_rows.scales) + scales_at(s.by_rows, row0, step, lane / kBlockLanes<T>);
+        if (row0 + 48u < s.rows) *(global_ptr<uint32_t>)to = scales;
+        else for (uint32_t q = 0; q < 4; ++q) if (row0 + q * 16u < s.rows) to[q] = (uint8_t)(scales >> (8u * q));
     }
 }
 
@@ -338,7 +331,7 @@ static void quantize_of(const LaunchCtx &lc, const MxSource &s)
         in_launches((tiles + kBlock / 64 - 1) / (kBlock / 64), [&](uint64_t first, uint32_t n) { launch(k, dim3(n), dim3(kBlock), lc.stream, s, first, tiles, steps); });
     } else {
         auto k = s.values ? mx_rows_k<T, true> : mx_rows_k<T, false>;
-        in_launches((uint64_t)((s.rows + 63u) / 64u) * steps, [&](uint64_t first, uint32_t n) { launch(k, dim3(n), dim3(kBlock), lc.stream, s, first, steps); });
+        in_launches((uint64_t)((s.rows + 63u) / 64u) * steps, [&](uint64_t first, uint32_t n) { launch(k, dim3(n), dim3(kRowsThreads<T>), lc.stream, s, first, steps); });
     }
 }
 void launch_mx_quantize(const LaunchCtx &lc, int dtype, const MxSource &s)
