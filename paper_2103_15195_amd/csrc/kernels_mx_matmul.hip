@@ -444,13 +444,16 @@ static bool lds_of(const LaunchCtx &lc, const MxProduct &p, uint64_t least)
 }
 // Which form takes a product (us, 16-bit results):
 //   256 x 256 outputs to a block    where that makes 110 blocks: 2048 x 2560 (80) over 4096 32 and 25 by the next form, 3328 x 2560 (130) over 2048 23 and 26
-//   128 x 128                       from 65 rows on: 128 x 4096 over 4096 11.3, and 14 to 20 by the next form, whose blocks read their operands so much oftener
-//   16 to 64 rows                   64 columns to a block where there are 200 such blocks (1 x 32064 over 4096 14.3, 5 TB/s), else 32 or 16: 16 x 4096 over
+//   128 x 128                       from 65 rows on, with more to do than 4800 steps of 64 x 16 outputs: 128 x 4096 over 4096 (16 384) 11.3, and 14 to 20 by the
+//                                   next form, 1024 x 1024 over 1024 (8192) 6.7 and 8.6, over 512 (4096) 6.0 and 5.3, 256 x 1000 over 2048 (4032) 8.7 and 6.2, 512 x
+//                                   512 over 512 (1024) 5.6 and 3.3
+//   straight from memory            64 columns to a block where there are 200 such blocks (1 x 32064 over 4096 14.3, 5 TB/s), else 32 or 16: 16 x 4096 over
 //                                   4096 7.0, and 10 with 64
 template <class T>
 static void matmul_of(const LaunchCtx &lc, const MxProduct &p)
 {
-    if (p.a.rows > 64u && (lds_of<T, 4, 1>(lc, p, 110u) || lds_of<T, 2, 2>(lc, p, 1u))) return;
+    const uint64_t much = (uint64_t)((p.a.rows + 63u) / 64u) * ((p.b.rows + 15u) / 16u) * p.a.steps;
+    if (p.a.rows > 64u && much > 4800u && (lds_of<T, 4, 1>(lc, p, 110u) || lds_of<T, 2, 2>(lc, p, 1u))) return;
     const bool wide = p.b.rows > 64u * 200u;
     if (p.a.rows <= 16u) {
         if (wide) few_of<T, 1, 4>(lc, p);

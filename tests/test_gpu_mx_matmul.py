@@ -54,7 +54,8 @@ def test_exact_sums(shape, dtype):
     h.close()
 
 
-@pytest.mark.parametrize("shape", [(5, 30, 40000), (40, 33, 50000), (70, 100, 20000), (130, 70, 9000), (2700, 2600, 300), (2817, 2561, 130), (9, 13000, 700), (30, 12900, 300), (50, 13001, 260)], ids=str)
+@pytest.mark.parametrize("shape", [(5, 30, 40000), (40, 33, 50000), (70, 100, 20000), (130, 70, 9000), (2700, 2600, 300), (2817, 2561, 130), (200, 330, 12000), (129, 4099, 1000), (1000, 1030, 1100), (9, 13000, 700),
+                                   (30, 12900, 300), (50, 13001, 260), (67, 12950, 100)], ids=str)
 def test_large_and_long(shape):
     """Sums that several blocks share, and outputs of many blocks, in each of the forms."""
     (m, n, k), h = shape, X.Mx()
@@ -91,7 +92,7 @@ def test_very_long_sums():
     torch.cuda.empty_cache()
 
 
-@pytest.mark.parametrize("shape", [(1, 70, 5000), (40, 70, 3000), (130, 260, 1500)], ids=str)
+@pytest.mark.parametrize("shape", [(1, 70, 5000), (40, 70, 2900), (130, 260, 1500), (300, 260, 9000), (3000, 2600, 600)], ids=str)
 def test_rounded_sums(shape):
     """Scales over a wide range.  Each of the steps' sums of 128 products and the additions that join them is off by at most a few units of its terms' size: a
     matrix instruction adds 128 products in at least seven levels and its result to a sum, so 8 roundings of up to 2^-23 each."""
@@ -112,7 +113,7 @@ def test_rounded_sums(shape):
 
 def test_blocks_that_stand_for_nan():
     """A NaN of a reaches its row, one of b its column, and nothing else."""
-    for m, n, k in ((3, 40, 300), (70, 300, 300), (300, 280, 200)):
+    for m, n, k in ((3, 40, 300), (70, 300, 300), (300, 280, 200), (600, 700, 1400), (2900, 2800, 600)):
         h, rng = X.Mx(), np.random.default_rng(9)
         a, b = grid(rng, m, k), grid(rng, n, k)
         x, y = a.to(DEV).float(), b.to(DEV).float()
@@ -146,7 +147,7 @@ def test_nothing_to_do():
 
 def test_same_bits_every_time():
     h, rng = X.Mx(), np.random.default_rng(3)
-    for m, n, k in ((1, 200, 20000), (30, 100, 9000), (200, 300, 5000)):
+    for m, n, k in ((1, 200, 20000), (30, 100, 9000), (200, 300, 5000), (300, 330, 12000)):
         x = torch.from_numpy(rng.standard_normal((m, k))).float().to(DEV)
         y = torch.from_numpy(rng.standard_normal((n, k))).float().to(DEV)
         A, Bm = X.MxMatrix(m, k), X.MxMatrix(n, k)
@@ -161,7 +162,7 @@ def test_same_bits_every_time():
 def test_on_a_stream_and_in_a_graph():
     """Captured products of several forms, replayed between eager ones on the same handle."""
     h, rng = X.Mx(), np.random.default_rng(4)
-    shapes = [(1, 300, 5000), (20, 70, 9000), (140, 300, 700)]
+    shapes = [(1, 300, 5000), (20, 70, 9000), (140, 300, 700), (200, 330, 12000)]
     mats = [(held(grid(rng, m, k)), held(grid(rng, n, k))) for m, n, k in shapes]
     outs = [torch.zeros(m, n, device=DEV) for m, n, _ in shapes]
     want = [torch.empty_like(o) for o in outs]
