@@ -26,7 +26,8 @@ extern "C" {
  * block.  The first moment is c s, the second (c s)^2: of it the root is held, which takes half the range of exponents.
  * After an update s is a block's largest magnitude / 448 and c = x / s rounded to nearest even, except that a root above 0 is never
  * rounded to 0, since updates are divided by it.  A block whose largest magnitude is below 2^-100 is held as zeros.  Infinities and NaN
- * leave the scale alone and are held as NaN, each in its own place.  Zero bytes and scales are moments of 0, which training begins with.
+ * leave the scale alone and are held as NaN, each in its own place, also where the rest of the block is held as zeros; the root of a square beyond
+ * binary32 is one of them, though its gradient is finite.  Zero bytes and scales are moments of 0, which training begins with.
  * (Nearest rounding holds an element's ratio to the largest of its block until it has changed by about a sixteenth; that largest itself
  * is followed in 32 bits.)
  */

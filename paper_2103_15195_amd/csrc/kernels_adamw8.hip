@@ -85,12 +85,14 @@ __device__ __forceinline__ float hold8(const float (&x)[8], codes8 &c)
     }
     top = row_max(top);
     const float scale = top >= 0x1p-100f ? top * (1.0f / 448.0f) : 0.0f, back = scale > 0.0f ? 1.0f / scale : 0.0f;
-    const float least = ROOT && scale > 0.0f ? 0x1p-9f : 0.0f;
+    // Roots above this are at least the least code: those above 0, and none in a block without a scale, where an infinity's 0 * infinity has to stay the NaN that it
+    // is (a maximum would drop it).
+    const float above = scale > 0.0f ? 0.0f : __builtin_huge_valf();
     float y[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         y[e] = x[e] * back;
-        if (ROOT) y[e] = x[e] > 0.0f ? fmaxf(y[e], least) : y[e];        // (not of a NaN, which is above nothing)
+        if (ROOT) y[e] = x[e] > above ? fmaxf(y[e], 0x1p-9f) : y[e];     // (not of a NaN, which is above nothing)
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {

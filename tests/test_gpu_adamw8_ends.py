@@ -1,0 +1,71 @@
+"""AdamW with moments in 8 bits at the ends of its range: blocks without a finite magnitude."""
+import math
+
+import pytest
+import torch
+
+from paper_2103_15195_amd import mx as X
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+BETAS = (0.9, 0.95)
+
+
+def from_nothing(grads, kind=torch.float32):
+    """(weights, their lists) after the first update of weights of 1, with these gradients."""
+    sizes = [g.numel() for g in grads]
+    h = X.Step8(sizes, kind)
+    lists = h.moments()
+    p = [torch.ones(n, device=DEV) for n in sizes]
+    h.bind(grads=grads, params=p, **lists)
+    h.mc_adamw8(1, 1e-2, BETAS)
+    h.close()
+    return p, lists
+
+
+def is_nan(code):
+    return code.cpu() & 127 == 127
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_blocks_of_nothing_finite(dtype, bad):
+    """A single element, one among zeros, one among what is held as zeros, a whole block, beside blocks that are as ever: NaN in its place, nothing in others', a scale of 0."""
+    kind = DTYPES[dtype]
+    small = 2.0 ** -120 if dtype == "f32" else 0.0           # (its root: below 2^-100)
+    grads = [torch.full((1,), bad), torch.zeros(300), torch.full((200,), small), torch.full((128 + 5,), bad), torch.ones(2049)]
+    grads[1][131], grads[2][7], grads[4][2048] = bad, bad, bad
+    p, lists = from_nothing([g.to(kind).to(DEV) for g in grads], kind)
+    for t, g in enumerate(grads):
+        finite = torch.isfinite(g)
+        for name in ("exp_avg", "exp_avg_sq"):
+            code, scale = lists[name][t], lists[name + "_scale"][t].cpu()
+            assert torch.equal(is_nan(code), ~finite), (t, name)
+            if t < 4:
+                assert bool((code.cpu()[finite] == 0).all()) and bool((scale == 0).all()), (t, name)
+            else:
+                assert bool((code.cpu()[finite] == 0x7E).all()) and bool((scale[:16] > 0).all()) and float(scale[16]) == 0, (t, name)
+        assert bool(torch.isfinite(p[t].cpu()[finite]).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_squares_beyond_the_range(dtype):
+    """Finite gradients whose squares are not: their roots are held as NaN and not as 0, so that no later update divides by next to nothing."""
+    kind = DTYPES[dtype]
+    grads = [torch.full((1,), 1e20), torch.full((128,), -1e20), torch.zeros(140), torch.ones(130)]
+    grads[2][139], grads[3][3] = 1e20, 1e20
+    p, lists = from_nothing([g.to(kind).to(DEV) for g in grads], kind)
+    for t, g in enumerate(grads):
+        large = g.abs() > 1e19
+        assert torch.equal(is_nan(lists["exp_avg_sq"][t]), large), t
+        assert not bool(is_nan(lists["exp_avg"][t]).any()), t
+        assert bool((p[t].cpu()[large] == 1).all()), t       # divided by an infinity
+    assert float(lists["exp_avg_sq_scale"][0]) == float(lists["exp_avg_sq_scale"][1]) == 0 and bool((lists["exp_avg_sq_scale"][2] == 0).all())
+    assert bool((lists["exp_avg_sq"][3].cpu()[[0, 1, 2, 4]] == 0x7E).all())
+    # the next gradients are ordinary: the weight says that its moments are lost
+    h = X.Step8([1], kind)
+    h.bind(grads=[torch.ones(1, dtype=kind, device=DEV)], params=p[:1], **{k: l[:1] for k, l in lists.items()})
+    h.mc_adamw8(2, 1e-2, BETAS)
+    assert math.isnan(float(p[0]))
+    h.close()
