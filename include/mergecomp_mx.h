@@ -28,8 +28,14 @@ extern "C" {
  * rounded to 0, since updates are divided by it.  A block whose largest magnitude is below 2^-100 is held as zeros.  Infinities and NaN
  * leave the scale alone and are held as NaN, each in its own place, also where the rest of the block is held as zeros; the root of a square beyond
  * binary32 is one of them, though its gradient is finite.  Zero bytes and scales are moments of 0, which training begins with.
- * (Nearest rounding holds an element's ratio to the largest of its block until it has changed by about a sixteenth; that largest itself
- * is followed in 32 bits.)
+ * What rounding takes away is not kept.  An update that changes an element's ratio to the largest of its block by less than half a step of its
+ * code (1/32 to 1/16 of it) leaves the code as it was, and such changes never add up; that largest itself is followed in 32 bits.  The first moment
+ * falls by 1 - beta1 of itself in an update, more than that at 0.9.  A root falls by no more than 1 - sqrt(beta2): 2.5 percent at 0.95, 0.05
+ * at 0.999.  Up to a beta2 of 0.98 the gradients' own variation, and the block's largest with it, moves codes often enough: after half of a block's normal
+ * gradients became four times smaller their roots were within -12 and +13 percent (0.95; 5th to 95th percentile) and -15 and +29 (0.98) of the
+ * true ones.  From 0.99 on roots do not come down: 2000 updates later they were 3 times the true ones (the median; 5000 later at 0.999 3.3), and
+ * updates that much too small; where gradients end altogether a root can stay for good.  Gradients that grow are followed.  With such a beta2
+ * take mc_adamw, whose moments have 32 bits, wherever gradients become smaller for long.
  */
 typedef struct mc_step8 mc_step8;
 

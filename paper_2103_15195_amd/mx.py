@@ -149,7 +149,10 @@ class Step8:
 
     def mc_adamw8(self, step: int, lr: float, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
                   coef=None, stream=None) -> None:
-        """coef: one float on the device that the gradients are multiplied by, such as the second of mc_grad_norm."""
+        """coef: one float on the device that the gradients are multiplied by, such as the second of mc_grad_norm.
+
+        Roots of second moments that become smaller are followed up to betas[1] of about 0.98.  With the default, AdamW's own, they stay where they were, several times
+        too large, and updates too small: what rounds to the same 8-bit code every time never adds up (the header has figures)."""
         rc = self._fast.adamw8(self._at, step, lr, betas[0], betas[1], eps, weight_decay, coef, B._raw_stream) if stream is None else None
         if rc is None:
             cfg = S.McAdamwConfig(lr, betas[0], betas[1], eps, weight_decay, step)
