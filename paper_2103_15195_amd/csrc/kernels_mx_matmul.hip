@@ -125,14 +125,15 @@ __device__ __forceinline__ rsrc_t buffer_at(const uint8_t *p, uint64_t bytes)
     return rsrc_t{(uint32_t)__builtin_amdgcn_readfirstlane((int)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)), (uint32_t)__builtin_amdgcn_readfirstlane((int)size), 0x00020000u};
 }
 // 16 (4) bytes a lane from its offset `from` to LDS at `to` + 16 (4) * lane.  The compiler does not count these loads: copied() waits.  (The whole offset
-// is the lane's: it is that which is checked against the buffer's size.)
+// is the lane's: it is that which is checked against the buffer's size.  LDS's place is in m0, which the compiler is told and writes itself; the wait behind
+// it is here, since it does not see what reads it.)
 __device__ __forceinline__ void copy16(uint32_t to, rsrc_t r, uint32_t from)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(from), "s"(r) : "memory");
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(to), "v"(from), "s"(r) : "memory");
 }
 __device__ __forceinline__ void copy4(uint32_t to, rsrc_t r, uint32_t from)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(from), "s"(r) : "memory");
+    asm volatile("s_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"{m0}"(to), "v"(from), "s"(r) : "memory");
 }
 // All but the last N of this wavefront's copies are done, and all that it has read from LDS is there; and the same of the block's other wavefronts.
 template <int N>
