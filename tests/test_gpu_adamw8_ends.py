@@ -1,9 +1,10 @@
-"""AdamW with moments in 8 bits at the ends of its range: blocks without a finite magnitude."""
+"""AdamW with moments in 8 bits at the ends of its range: blocks without a finite magnitude, weights among the smallest and largest gradients."""
 import math
 
 import pytest
 import torch
 
+import mx_reference as R
 from paper_2103_15195_amd import mx as X
 
 pytestmark = pytest.mark.gpu
@@ -68,4 +69,26 @@ def test_squares_beyond_the_range(dtype):
     h.bind(grads=[torch.ones(1, dtype=kind, device=DEV)], params=p[:1], **{k: l[:1] for k, l in lists.items()})
     h.mc_adamw8(2, 1e-2, BETAS)
     assert math.isnan(float(p[0]))
+    h.close()
+
+
+@pytest.mark.parametrize("size", [1e-34, 1e-28, 1e15, 1e18])
+def test_weights_of_very_small_and_very_large_gradients(size):
+    """Weights within what 32-bit arithmetic may be off by, second moments that may count as 0 (the least of them) among it."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(11)
+    sizes, hyper = [1, 129, 2048, 2049 + 131], dict(lr=1e-2, betas=BETAS, eps=1e-8, weight_decay=0.1)
+    normal = lambda n: torch.randn(n, device=DEV, generator=gen)  # noqa: E731
+    h = X.Step8(sizes)
+    lists = h.moments()
+    p, g = [normal(n) for n in sizes], [0.3 * size * normal(n) for n in sizes]
+    h.bind(grads=g, params=p, **lists)
+    for step in (1, 2, 3):
+        want = [R.adamw8(a, b, c, d, e, f, 1.0, step, hyper["lr"], hyper["betas"], hyper["eps"], hyper["weight_decay"]) for a, b, c, d, e, f in
+                zip(p, lists["exp_avg"], lists["exp_avg_scale"], lists["exp_avg_sq"], lists["exp_avg_sq_scale"], g)]
+        h.mc_adamw8(step, **hyper)
+        for t, ((pw, _, _), (off, _, _)) in enumerate(want):
+            assert bool(((p[t].cpu().double() - pw).abs() <= off).all()), (step, t)
+        for x, n in zip(g, sizes):
+            x.copy_(0.3 * size * normal(n))
     h.close()
