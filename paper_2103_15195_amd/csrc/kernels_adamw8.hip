@@ -108,8 +108,9 @@ __device__ __forceinline__ global_ptr<T> list8(const Step8View &v, uint32_t list
 {
     return in_global(reinterpret_cast<T *>(ld_uniform(v.addr + (size_t)list * v.tensors + tensor)));
 }
-// The square root, rounded correctly from 2^-96 on (below, by up to a unit in the last place): the hardware's, or the number on either side of it where
-// the square of half way to that one says so.
+// The square root, rounded correctly from 2^-96 on (below, by up to a unit in the last place), by Tuckerman's test (Agarwal et al., New scalar and vector elementary functions for the
+// IBM System/370, 1986): s, off by at most a unit u, is the root's rounding where s (s - u) < x <= s (s + u), else it is the neighbour on that side.  A fused multiply-add has the
+// sign of either difference without an error.
 __device__ __forceinline__ float root_of(float x)
 {
     const float s = __builtin_amdgcn_sqrtf(x);

@@ -114,7 +114,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void mx_matmul_few_k(MxProduct p, u
 // ---- many rows -----------------------------------------------------------------------------------------------------------
 // Operands through LDS: four wavefronts have 64 PA x 64 PB outputs, each a quarter of them.  A step's codes and scales are copied straight to LDS, three steps
 // ahead; a wavefront reads the operands of the next half step while it multiplies this one's.  With GROUPS = 2 a block has two such fours, which take
-// half of the steps each.  256 x 256 outputs over 4096 to a block and 128 x 128 read 31 and 62 bytes of operands for a thousand products; a step of 128 takes a block of
+// half of the steps each.  256 x 256 outputs to a block and 128 x 128 read 4.2 and 8.3 bytes of operands for a thousand products (17/32 a value); a step of 128 takes a block of
 // the first kind 0.9 us (a third of it waits; the clock falls to 1.6 GHz), of the second 0.39 for both of its groups.
 typedef uint32_t rsrc_t __attribute__((ext_vector_type(4)));
 // What a buffer's loads go by: beyond `bytes` they give 0.
@@ -403,8 +403,9 @@ static void shared_by(const LaunchCtx &lc, const MxProduct &p, uint32_t splits, 
 
 // How many blocks share a tile's steps: the power of two whose estimate is the shortest, from what was measured: 3 us for a round of 256 blocks to begin and end,
 // `step` us for each of its steps; for the parts' pass 3 us, and 2 us for a million of their elements.  (512 x 1024 outputs over 12 544: 24.8 us
-// without splits, 16.1 with eight; 256 x 256 over 65 536 104 and 21.6; 2048 x 2048 over 4096 14.7 with none.  Parts that the last block of a tile to come adds
-// up, through memory and counts, took 25 us for the first.)
+// without splits, 15.5 with the four that this takes; 256 x 256 over 65 536 104 and 21.4; 2048 x 2048 over 4096 14.7 with none.  Parts that the last block of a tile to come adds
+// up, through memory and counts, took 25 us for the first.  Its estimate is 15.2, but 8.0 for the product, which takes 12.3, and 7.2 for the parts' pass, which takes
+// 4.0: that every die fetches all of a, 36 MB together where the operands have 10, is not in it.)
 static uint32_t splits_for(const MxProduct &p, uint64_t tiles, double step)
 {
     const uint64_t part = (uint64_t)p.a.rows * ((p.b.rows + 3u) / 4u * 4u);
@@ -448,8 +449,13 @@ static bool lds_of(const LaunchCtx &lc, const MxProduct &p, uint64_t least)
 //   128 x 128                       from 65 rows on, with more to do than 4800 steps of 64 x 16 outputs: 128 x 4096 over 4096 (16 384) 11.3, and 14 to 20 by the
 //                                   next form, 1024 x 1024 over 1024 (8192) 6.7 and 8.6, over 512 (4096) 6.0 and 5.3, 256 x 1000 over 2048 (4032) 8.7 and 6.2, 512 x
 //                                   512 over 512 (1024) 5.6 and 3.3
-//   straight from memory            64 columns to a block where there are 200 such blocks (1 x 32064 over 4096 14.3, 5 TB/s), else 32 or 16: 16 x 4096 over
-//                                   4096 7.0, and 10 with 64
+//   straight from memory            64 columns to a block above 12 800 of them (more than 200 such blocks: 1 x 32064 over 4096 13.6, 5 TB/s), else 16, or for up to 16 rows 32
+//                                   above 6400: 16 x 4096 over 4096 7.0, and 10 with 64
+// Both sides of the border of 12 800, over 4096 (three sets of operands in turn, which the last-level cache holds): 16 rows by 12 736 and 12 800 (400 blocks of 32 columns) 8.0 to 8.7
+// and by 12 864 (201 of 64) 8.9; 17, 32 and 64 rows by 12 800 (800 of 16) 11.2, 11.5 and 15.9, by 12 864 9.1, 9.2 and 10.7: for more than 16 rows it lies too high.  (By 8192: 7.3, 7.7
+// and 9.1.)
+// The count of 256 x 256 blocks takes them as full: 65, 128, 192 and 256 rows by 32 064 over 4096, 126 blocks that are a quarter to wholly filled, take 31.4, 35.1, 35.2
+// and 35.3, where the bytes are 14 to 17's; 512 x 16 384 27.7, 32 064 x 128 29.6.
 template <class T>
 static void matmul_of(const LaunchCtx &lc, const MxProduct &p)
 {
