@@ -7,8 +7,10 @@
  *
  * Conventions: those of mergecomp_step.h.  A handle belongs to the device that was current when it was made, calls only enqueue kernels
  * on the caller's stream, allocate nothing and never synchronise, and all calls on one handle are issued in stream order, since they
- * share its scratch (calls captured into graphs too: graphs that hold calls on one handle are not replayed at the same time).  The same
- * call gives the same bits.  What a call writes may not lie over anything else that it writes or reads.
+ * share its scratch (calls captured into graphs too: graphs that hold calls on one handle are not replayed at the same time).  A captured
+ * call keeps the numbers that it was made with (an update's step and rate too) and goes by the lists that are bound when it is replayed: the handle, what is
+ * bound and the matrices have to be there until the last replay.  The same call gives the same bits.  What a call writes may not lie over anything else that it
+ * writes or reads.
  */
 #ifndef MERGECOMP_MX_H
 #define MERGECOMP_MX_H

@@ -78,7 +78,7 @@ def _fast(device):
 
 class Step8:
     """One model's list of tensors whose moments are held in 8 bits, on the current device: wraps mc_step8.  All that is handed over later has to
-    be on that device.
+    be on that device.  A graph that holds its calls is replayed only while it lives, with the numbers (step, lr, ...) that they were captured with.
 
     grad_dtype   type of the gradients
     model_dtype  type of the copy of the weights that the model computes with, or None for no such copy
@@ -120,7 +120,7 @@ class Step8:
             pass
 
     def moments(self) -> dict:
-        """The four lists of moments of a training that begins: zeros on the handle's device, in the form that bind() takes."""
+        """The four lists of moments of a training that begins: zeros on the handle's device, written on torch's current stream, in the form that bind() takes."""
         blocks = [(n + BLOCK8 - 1) // BLOCK8 for n in self.numel]
         return {name: [torch.zeros(n, dtype=self.dtypes[name], device=self._device) for n in (blocks if name.endswith("scale") else self.numel)]
                 for name in ("exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale")}
@@ -162,8 +162,8 @@ class Step8:
 
 
 class MxMatrix:
-    """rows x cols values in microscaled 4-bit floating point: the two buffers of mc_mx_matrix, made here (on the current device) or
-    handed over (bytes, contiguous, on one device, mc_mx_code_bytes and mc_mx_scale_bytes of them).  A matrix keeps its buffers: another one's are another matrix."""
+    """rows x cols values in microscaled 4-bit floating point: the two buffers of mc_mx_matrix, made here (zeros on the current device, written on torch's current
+    stream, which calls on another one have to wait for) or handed over (bytes, contiguous, on one device, mc_mx_code_bytes and mc_mx_scale_bytes of them).  A matrix keeps its buffers: another one's are another matrix."""
 
     rows = property(lambda self: self._rows)
     cols = property(lambda self: self._cols)
@@ -197,7 +197,8 @@ def _matrix(m, name: str, device, rows=None, cols=None):
 
 
 class Mx:
-    """Scratch of the calls over quantised matrices, on the current device, where their tensors have to be: wraps mc_mx."""
+    """Scratch of the calls over quantised matrices, on the current device, where their tensors have to be: wraps mc_mx.  A graph that holds its calls is replayed only
+    while it lives."""
 
     def __init__(self):
         self._h = C.c_void_p()
